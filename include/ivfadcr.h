@@ -253,6 +253,52 @@ int ivfr_workspace_info(const ivfr_index* index, int64_t* index_bytes, int64_t* 
 int ivfr_set_profiling(ivfr_index* index, int32_t enable);
 int ivfr_stage_times(const ivfr_index* index, double* ms, int32_t* scan_launches);
 
+/* Learning the vectors.  An index holds vectors that some model made; the two operators below train such a model's last
+ * matrix, or a table of vectors, on the GPU that searches them: the softmax loss of rows against a large set of vectors with
+ * its gradient, and the orthogonalised update that is made of a matrix's gradient.
+ *
+ * They belong to no index.  Inputs, outputs and workspace are the caller's device memory on args->device; inputs and outputs
+ * must not overlap.  Calls are enqueued on `stream` and return without waiting; nothing is allocated or read back, so they can
+ * be captured in a graph, and calls with different workspaces may overlap.  *_workspace is host arithmetic: the bytes that
+ * the call with these arguments needs (aligned to 256).  Matrices are row-major with a leading dimension in elements; inputs
+ * may start anywhere that their type allows (rows of 16-byte alignment are read in place, others copied).
+ * Sums and statistics are fp32.  Products of bf16 and fp16 inputs are exact; fp32 inputs are split into three bf16 parts, whose
+ * six leading products neglect 2^-24 of a product.  Errors: IVFR_ERR_INVALID_ARG, IVFR_ERR_HIP. */
+#define IVFR_TYPE_F32  0
+#define IVFR_TYPE_F16  1
+#define IVFR_TYPE_BF16 2
+
+/* Softmax cross entropy without keeping the n x v scores z_ij = scale * x_i . w_j + offset_j.
+ *   lse_i  = log sum_j exp z_ij;   loss_i = lse_i - z_i,target(i)
+ *   e_ij   = weight_i (exp(z_ij - lse_i) - [j = target(i)]);   dx = scale e w;   dw = scale e^T x
+ * targets int64: a negative one marks a row without a target (loss 0, no gradient whatever x_i holds; its lse is that of its scores); one of v or more makes the row's loss,
+ * and the gradients that it enters, NaN.  offset (may be NULL): a constant per vector, as the negative logarithm of how often it was drawn;
+ * no gradient is formed for it.  -INFINITY leaves the vector out, whatever w_j holds: it gets a zero gradient, a row whose target it is
+ * the loss +INFINITY.  A row with every vector left out has lse -INFINITY and no gradient.  Other components must be finite,
+ * else losses and gradients that they enter are not numbers.
+ * ivfr_softmax_loss: loss, lse fp32 [n].
+ * ivfr_softmax_loss_grad: weight fp32 [n], the gradient of each row's loss; lse fp32 [n] of ivfr_softmax_loss for these arguments, or NULL
+ * (it is then formed here); loss fp32 [n], or NULL; dx [n, d] and dw [v, d] dense, of the inputs' type, aligned to 16 bytes.
+ * fp16 gradients below 2^-24 are zero in that type: scale the weights as for any training in fp16.  The order of every sum is fixed:
+ * the same call gives the same bits. */
+typedef struct {
+    int64_t n, v;            /* rows; vectors                                                */
+    int32_t d;               /* components of both                                           */
+    int32_t type;            /* IVFR_TYPE_* of x, w, dx, dw                                  */
+    const void* x;           /* [n, d]                                                       */
+    int64_t ldx;
+    const void* w;           /* [v, d]                                                       */
+    int64_t ldw;
+    const int64_t* targets;  /* [n]                                                          */
+    const float* offset;     /* [v] or NULL                                                  */
+    float scale;
+    int32_t device;          /* HIP device ordinal                                           */
+} ivfr_softmax_args;
+int ivfr_softmax_workspace(const ivfr_softmax_args* args, int32_t grad, int64_t* bytes);
+int ivfr_softmax_loss(const ivfr_softmax_args* args, float* loss, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+int ivfr_softmax_loss_grad(const ivfr_softmax_args* args, const float* weight, const float* lse, float* loss, void* dx, void* dw,
+                           void* workspace, int64_t workspace_bytes, void* stream);
+
 const char* ivfr_last_error(void);
 
 #ifdef __cplusplus

@@ -30,6 +30,12 @@ class Params(ctypes.Structure):
                 ("m_refine", ctypes.c_int32), ("device", ctypes.c_int32)]
 
 
+class SoftmaxArgs(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("v", ctypes.c_int64), ("d", ctypes.c_int32), ("type", ctypes.c_int32),
+                ("x", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("w", ctypes.c_void_p), ("ldw", ctypes.c_int64),
+                ("targets", ctypes.c_void_p), ("offset", ctypes.c_void_p), ("scale", ctypes.c_float), ("device", ctypes.c_int32)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run `python -m paper_1102_3828_amd.build` "
@@ -60,6 +66,9 @@ def _load():
         "ivfr_set_memory_limit": (ctypes.c_int, [vp, i64]),
         "ivfr_workspace_info": (ctypes.c_int, [vp] + [ctypes.POINTER(i64)] * 4),
         "ivfr_stage_times": (ctypes.c_int, [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i32)]),
+        "ivfr_softmax_workspace": (ctypes.c_int, [ctypes.POINTER(SoftmaxArgs), i32, ctypes.POINTER(i64)]),
+        "ivfr_softmax_loss": (ctypes.c_int, [ctypes.POINTER(SoftmaxArgs), vp, vp, vp, i64, vp]),
+        "ivfr_softmax_loss_grad": (ctypes.c_int, [ctypes.POINTER(SoftmaxArgs), vp, vp, vp, vp, vp, vp, i64, vp]),
         "ivfr_last_error": (ctypes.c_char_p, []),
     }
     for name, (res, args) in sig.items():
@@ -72,7 +81,8 @@ lib = _load()
 EXPORTED = ["ivfr_create", "ivfr_destroy", "ivfr_train", "ivfr_set_codebooks", "ivfr_get_codebooks", "ivfr_add",
             "ivfr_finalize", "ivfr_ntotal", "ivfr_export", "ivfr_import", "ivfr_search", "ivfr_search_static", "ivfr_search_trace",
             "ivfr_search_stats", "ivfr_set_list_sharing", "ivfr_set_tuning", "ivfr_set_profiling", "ivfr_stage_times", "ivfr_last_error",
-            "ivfr_memory_required", "ivfr_set_memory_limit", "ivfr_workspace_info", "ivfr_set_table_mode"]
+            "ivfr_memory_required", "ivfr_set_memory_limit", "ivfr_workspace_info", "ivfr_set_table_mode",
+            "ivfr_softmax_workspace", "ivfr_softmax_loss", "ivfr_softmax_loss_grad"]
 
 
 def _check(rc):
@@ -264,3 +274,114 @@ class Index:
         out = dict(zip(self.STAGES, [float(v) for v in ms]))
         out["scan_launches"] = n.value
         return out
+
+
+# ---- learning the vectors (include/ivfadcr.h): operators on the caller's tensors, without an index
+
+_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+class _Call:
+    """The stream of a call, and the tensors it needs allocated for that stream (they may be freed while the call is still under way)."""
+
+    def __init__(self, device, stream):
+        self.device = device
+        self.stream = torch.cuda.current_stream(device) if stream is None else torch.cuda.ExternalStream(stream, device=device)
+
+    def __enter__(self):
+        self._guard = torch.cuda.stream(self.stream)
+        self._guard.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        return self._guard.__exit__(*exc)
+
+    @property
+    def handle(self):
+        return ctypes.c_void_p(self.stream.cuda_stream)
+
+    def empty(self, shape, dtype):
+        return torch.empty(shape, dtype=dtype, device=self.device)
+
+
+def _rows(a, name):
+    """A matrix of a supported type whose rows are contiguous (they may lie further apart than their length)."""
+    if a.dim() != 2 or a.dtype not in _TYPES or not a.is_cuda:
+        raise ValueError(f"{name} must be a float32, float16 or bfloat16 matrix on the GPU")
+    if a.shape[0] <= 1:
+        return a.contiguous(), max(a.shape[1], 1)
+    if a.shape[1] > 1 and a.stride(1) != 1 or a.stride(0) < a.shape[1]:
+        a = a.contiguous()
+    return a, a.stride(0)
+
+
+def _softmax_args(x, w, targets, scale, offset):
+    x, ldx = _rows(x, "x")
+    w, ldw = _rows(w, "w")
+    n, d = x.shape
+    if w.shape[1] != d or w.dtype != x.dtype or w.device != x.device:
+        raise ValueError("x and w must have the same number of components, type and device")
+    if targets.shape != (n,) or targets.dtype not in (torch.int64, torch.int32) or targets.device != x.device:
+        raise ValueError("targets must be int64 or int32 [n] on the device of x")
+    targets = targets.to(torch.int64).contiguous()
+    if offset is not None:
+        if offset.shape != (w.shape[0],) or offset.dtype != torch.float32 or offset.device != x.device:
+            raise ValueError("offset must be float32 [v] on the device of x")
+        offset = offset.contiguous()
+    args = SoftmaxArgs(n, w.shape[0], d, _TYPES[x.dtype], x.data_ptr(), ldx, w.data_ptr(), ldw, targets.data_ptr(),
+                       None if offset is None else offset.data_ptr(), float(scale), x.device.index)
+    return args, (x, w, targets, offset)   # (the tensors that the addresses belong to)
+
+
+def _softmax_workspace(args, grad, call):
+    need = ctypes.c_int64()
+    _check(lib.ivfr_softmax_workspace(ctypes.byref(args), int(grad), ctypes.byref(need)))
+    return call.empty(need.value, torch.uint8), need.value
+
+
+def softmax_loss(x, w, targets, scale=1.0, offset=None, stream=None):
+    """Softmax cross entropy of the rows x [n, d] against the vectors w [v, d] (float32, float16 or bfloat16), without keeping the n x v
+    scores scale * x w^T + offset.  targets: int64 or int32 [n], negative for rows without one.  offset: float32 [v] or None; -inf
+    leaves a vector out.  Returns (loss, lse), float32 [n]; include/ivfadcr.h has the definitions."""
+    with _Call(x.device, stream) as call:
+        args, keep = _softmax_args(x, w, targets, scale, offset)
+        ws, size = _softmax_workspace(args, False, call)
+        loss, lse = call.empty((args.n,), torch.float32), call.empty((args.n,), torch.float32)
+        _check(lib.ivfr_softmax_loss(ctypes.byref(args), _ptr(loss), _ptr(lse), _ptr(ws), size, call.handle))
+    return loss, lse
+
+
+def softmax_loss_grad(x, w, targets, weight, scale=1.0, offset=None, lse=None, stream=None):
+    """The gradients of sum_i weight_i loss_i.  weight: float32 [n].  Returns (loss, dx, dw), dx and dw of the inputs' type; with lse
+    (of softmax_loss for the same arguments) given, the statistics are not formed again and loss is None."""
+    with _Call(x.device, stream) as call:
+        args, keep = _softmax_args(x, w, targets, scale, offset)
+        n, v, d = args.n, args.v, args.d
+        for t, name in ((weight, "weight"), (lse, "lse")):
+            if t is not None and (t.shape != (n,) or t.dtype != torch.float32 or t.device != x.device):
+                raise ValueError(f"{name} must be float32 [n] on the device of x")
+        weight = weight.contiguous()
+        lse = None if lse is None else lse.contiguous()
+        ws, size = _softmax_workspace(args, True, call)
+        loss = call.empty((n,), torch.float32) if lse is None else None
+        dx, dw = call.empty((n, d), x.dtype), call.empty((v, d), x.dtype)
+        _check(lib.ivfr_softmax_loss_grad(ctypes.byref(args), _ptr(weight), _ptr(lse), _ptr(loss), _ptr(dx), _ptr(dw), _ptr(ws), size,
+                                          call.handle))
+    return loss, dx, dw
+
+
+class SoftmaxLoss(torch.autograd.Function):
+    """softmax_loss for autograd: SoftmaxLoss.apply(x, w, targets, scale, offset) is the loss of each row; gradients go to x and w."""
+
+    @staticmethod
+    def forward(ctx, x, w, targets, scale=1.0, offset=None):
+        loss, lse = softmax_loss(x, w, targets, scale, offset)
+        ctx.save_for_backward(x, w, targets, lse, offset)
+        ctx.scale = scale
+        return loss
+
+    @staticmethod
+    def backward(ctx, grad):
+        x, w, targets, lse, offset = ctx.saved_tensors
+        _, dx, dw = softmax_loss_grad(x, w, targets, grad.to(torch.float32), ctx.scale, offset, lse)
+        return dx, dw, None, None, None
