@@ -299,6 +299,28 @@ int ivfr_softmax_loss(const ivfr_softmax_args* args, float* loss, float* lse, vo
 int ivfr_softmax_loss_grad(const ivfr_softmax_args* args, const float* weight, const float* lse, float* loss, void* dx, void* dw,
                            void* workspace, int64_t workspace_bytes, void* stream);
 
+/* Orthogonalised update of matrices g [batch][rows, cols] (a projection's gradient or momentum) by Newton-Schulz products:
+ *   X = g / (||g||_F + eps);  per step  A = X X^T,  X <- a X + (b A + c A^2) X;  out = scale X
+ * (with the shorter side as the rows of X).  out is close to the nearest matrix of orthonormal rows or columns: singular vectors stay, a
+ * singular value s becomes a s + b s^3 + c s^5 in each step.  coefficients: host fp32 [steps][3] of (a, b, c); refused
+ * (IVFR_ERR_INVALID_ARG) when singular values of up to 1 would leave (-15, 15) under them.  (3.4445, -4.7750, 2.0315), five times,
+ * takes values from 0.01 to 1 into 0.7 to 1.2.  The products of bf16 and fp16 matrices are formed in fp16 at a fixed scale, with 11 bits
+ * of every number of X, A and B; those of fp32 matrices with 22 bits.  A matrix of zeros stays zero (eps > 0); what is not finite makes its
+ * matrix NaN.  out: dense [batch][rows, cols], of the type of g.  The order of every sum is fixed. */
+typedef struct {
+    int64_t batch;               /* at most 65535                                            */
+    int32_t rows, cols;          /* at most 2^20, the shorter at most 2^16                   */
+    int32_t type;                /* IVFR_TYPE_* of g and out                                 */
+    int32_t steps;               /* 1 to 64                                                  */
+    const void* g;
+    int64_t ld, batch_stride;    /* elements between rows, between matrices                  */
+    const float* coefficients;   /* host                                                     */
+    float scale, eps;
+    int32_t device;
+} ivfr_orthogonalize_args;
+int ivfr_orthogonalize_workspace(const ivfr_orthogonalize_args* args, int64_t* bytes);
+int ivfr_orthogonalize(const ivfr_orthogonalize_args* args, void* out, void* workspace, int64_t workspace_bytes, void* stream);
+
 const char* ivfr_last_error(void);
 
 #ifdef __cplusplus

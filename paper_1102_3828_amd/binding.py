@@ -36,6 +36,12 @@ class SoftmaxArgs(ctypes.Structure):
                 ("targets", ctypes.c_void_p), ("offset", ctypes.c_void_p), ("scale", ctypes.c_float), ("device", ctypes.c_int32)]
 
 
+class OrthogonalizeArgs(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("type", ctypes.c_int32), ("steps", ctypes.c_int32),
+                ("g", ctypes.c_void_p), ("ld", ctypes.c_int64), ("batch_stride", ctypes.c_int64), ("coefficients", ctypes.c_void_p),
+                ("scale", ctypes.c_float), ("eps", ctypes.c_float), ("device", ctypes.c_int32)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run `python -m paper_1102_3828_amd.build` "
@@ -69,6 +75,8 @@ def _load():
         "ivfr_softmax_workspace": (ctypes.c_int, [ctypes.POINTER(SoftmaxArgs), i32, ctypes.POINTER(i64)]),
         "ivfr_softmax_loss": (ctypes.c_int, [ctypes.POINTER(SoftmaxArgs), vp, vp, vp, i64, vp]),
         "ivfr_softmax_loss_grad": (ctypes.c_int, [ctypes.POINTER(SoftmaxArgs), vp, vp, vp, vp, vp, vp, i64, vp]),
+        "ivfr_orthogonalize_workspace": (ctypes.c_int, [ctypes.POINTER(OrthogonalizeArgs), ctypes.POINTER(i64)]),
+        "ivfr_orthogonalize": (ctypes.c_int, [ctypes.POINTER(OrthogonalizeArgs), vp, vp, i64, vp]),
         "ivfr_last_error": (ctypes.c_char_p, []),
     }
     for name, (res, args) in sig.items():
@@ -82,7 +90,8 @@ EXPORTED = ["ivfr_create", "ivfr_destroy", "ivfr_train", "ivfr_set_codebooks", "
             "ivfr_finalize", "ivfr_ntotal", "ivfr_export", "ivfr_import", "ivfr_search", "ivfr_search_static", "ivfr_search_trace",
             "ivfr_search_stats", "ivfr_set_list_sharing", "ivfr_set_tuning", "ivfr_set_profiling", "ivfr_stage_times", "ivfr_last_error",
             "ivfr_memory_required", "ivfr_set_memory_limit", "ivfr_workspace_info", "ivfr_set_table_mode",
-            "ivfr_softmax_workspace", "ivfr_softmax_loss", "ivfr_softmax_loss_grad"]
+            "ivfr_softmax_workspace", "ivfr_softmax_loss", "ivfr_softmax_loss_grad",
+            "ivfr_orthogonalize_workspace", "ivfr_orthogonalize"]
 
 
 def _check(rc):
@@ -385,3 +394,30 @@ class SoftmaxLoss(torch.autograd.Function):
         x, w, targets, lse, offset = ctx.saved_tensors
         _, dx, dw = softmax_loss_grad(x, w, targets, grad.to(torch.float32), ctx.scale, offset, lse)
         return dx, dw, None, None, None
+
+
+def orthogonalize(g, steps=5, coefficients=(3.4445, -4.7750, 2.0315), scale=1.0, eps=1e-7, stream=None):
+    """The orthogonalised update of g [rows, cols] or [batch, rows, cols] (float32, float16 or bfloat16) by Newton-Schulz products: a
+    matrix of the same singular vectors whose singular values are near `scale`.  coefficients: (a, b, c), or one such triple per step.
+    The result is dense, of the shape and type of g."""
+    if g.dim() not in (2, 3) or g.dtype not in _TYPES or not g.is_cuda:
+        raise ValueError("g must be a float32, float16 or bfloat16 matrix, or a batch of them, on the GPU")
+    flat = [float(x) for k in coefficients for x in (k if hasattr(k, "__len__") else (k,))]
+    if len(flat) == 3:
+        flat = flat * int(steps)
+    if len(flat) != 3 * int(steps):
+        raise ValueError("coefficients must be (a, b, c), or one such triple per step")
+    with _Call(g.device, stream) as call:
+        m = g if g.dim() == 3 else g[None]
+        b, rows, cols = m.shape
+        ld, each = m.stride(1) if rows > 1 else cols, m.stride(0) if b > 1 else rows * cols
+        if (cols > 1 and m.stride(2) != 1) or ld < cols or each < (rows - 1) * ld + cols:
+            m, ld, each = m.contiguous(), cols, rows * cols
+        coef = (ctypes.c_float * len(flat))(*flat)
+        args = OrthogonalizeArgs(b, rows, cols, _TYPES[g.dtype], int(steps), m.data_ptr(), ld, each, ctypes.cast(coef, ctypes.c_void_p),
+                                 float(scale), float(eps), g.device.index)
+        need = ctypes.c_int64()
+        _check(lib.ivfr_orthogonalize_workspace(ctypes.byref(args), ctypes.byref(need)))
+        ws, out = call.empty(need.value, torch.uint8), call.empty(tuple(g.shape), g.dtype)
+        _check(lib.ivfr_orthogonalize(ctypes.byref(args), _ptr(out), _ptr(ws), need.value, call.handle))
+    return out

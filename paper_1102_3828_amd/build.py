@@ -14,7 +14,7 @@ SYNTH_SRC = os.path.join(ROOT, "synthdata", "gen.hip")
 SYNTH_LIB = os.path.join(ROOT, "synthdata", "libsynthgen.so")
 
 SOURCES = ["index.hip", "gemm.hip", "select.hip", "scan.hip", "bound.hip", "scan_select.hip", "rerank.hip", "encode.hip", "search.hip",
-           "product.hip", "softmax.hip"]
+           "product.hip", "softmax.hip", "ortho.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]

@@ -1,0 +1,408 @@
+// Orthogonalised update of matrices g [rows, cols] by Newton-Schulz products:
+//
+//   X = g / (||g||_F + eps);   per step  A = X X^T,  B = b A + c A^2,  X <- a X + B X;   out = scale X
+//
+// with the shorter side as X's rows (a tall matrix is transposed when it is read and written).  The singular vectors stay, a
+// singular value s becomes a s + b s^3 + c s^5 a step.
+//
+// Every number of X, A and B is bounded by the singular values (which the coefficients keep in range, checked by the host), so the products run in
+// fp16 at a fixed scale of 2^12: three more bits than bf16 at the same rate, and values down to 2^-26 of the largest keep them all.
+// fp32 matrices are carried by two fp16 planes (22 bits and a sign), three products.  A and A^2 are symmetric: the tiles on and below the
+// diagonal are formed and written twice.  Sums are fp32; X, A and B are rounded once per product, to the planes that the next one reads.
+// All sides are padded with zeros to whole stages of 32.
+#include "product.h"
+
+#include <algorithm>
+#include <cmath>
+
+#define ORTHO_SCALE 4096.f
+#define ORTHO_SUMS 64          // workgroups that sum the squares of a matrix
+
+struct OrthoPlan {
+    int r, c, rp, cp, planes;
+    bool tall, half;
+    int64_t batch;
+    int64_t at_sums, at_x[2], at_a, at_b, bytes;
+    int64_t xsize, asize;      // elements of a plane of one matrix
+};
+
+struct MatrixArgs {
+    const void* g;
+    int64_t ld, batch_stride;
+    int rows, cols, type;      // of g
+    int tall, rp, cp, planes;
+    int64_t xsize;             // elements of a plane; a matrix has `planes` of them
+    float eps;
+    double* sums;              // [batch][ORTHO_SUMS]
+    uint16_t* x;
+    void* out;                 // dense, as g
+    float out_scale;
+};
+
+__device__ __forceinline__ float load_value(const void* p, int64_t at, int type) {
+    if (type == IVFR_TYPE_F32) return ((const float*)p)[at];
+    const uint16_t h = ((const uint16_t*)p)[at];
+    return type == IVFR_TYPE_F16 ? from_half(h) : from_bf16(h);
+}
+__device__ __forceinline__ void store_value(void* p, int64_t at, int type, float v) {
+    if (type == IVFR_TYPE_F32) ((float*)p)[at] = v;
+    else ((uint16_t*)p)[at] = type == IVFR_TYPE_F16 ? to_half(v) : to_bf16(v);
+}
+// one value into its planes
+__device__ __forceinline__ void store_planes(uint16_t* p, int64_t plane, int planes, float v) {
+    const uint16_t h = to_half(v);
+    p[0] = h;
+    if (planes > 1) p[plane] = to_half(v - from_half(h));
+}
+__device__ __forceinline__ float load_planes(const uint16_t* p, int64_t plane, int planes) { return from_half(p[0]) + (planes > 1 ? from_half(p[plane]) : 0.f); }
+
+// Sums of squares, in fp64 (squares of fp32 values need not fit fp32), in a fixed order.
+__global__ __launch_bounds__(256) void squares_kernel(MatrixArgs a) {
+    __shared__ double red[4];
+    const int64_t total = (int64_t)a.rows * a.cols, base = (int64_t)blockIdx.y * a.batch_stride;
+    double s = 0.0;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += ORTHO_SUMS * 256) {
+        const int64_t row = i / a.cols;
+        const double v = load_value(a.g, base + row * a.ld + (i - row * a.cols), a.type);
+        s += v * v;
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off, 64);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) a.sums[(int64_t)blockIdx.y * ORTHO_SUMS + blockIdx.x] = red[0] + red[1] + red[2] + red[3];
+}
+
+// 64 x 64 values of X, through LDS where g is transposed
+__global__ __launch_bounds__(256) void fill_kernel(MatrixArgs a) {
+    __shared__ float tile[64][65];
+    __shared__ double inv_s;
+    if (threadIdx.x < 64) {
+        double s = a.sums[(int64_t)blockIdx.z * ORTHO_SUMS + threadIdx.x];
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off, 64);
+        if (threadIdx.x == 0) inv_s = (double)ORTHO_SCALE / (sqrt(s) + (double)a.eps);
+    }
+    __syncthreads();
+    const double inv = inv_s;
+    const int c0 = blockIdx.x * 64, r0 = blockIdx.y * 64, r = a.tall ? a.cols : a.rows, c = a.tall ? a.rows : a.cols;
+    const int64_t base = (int64_t)blockIdx.z * a.batch_stride;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (a.tall) {
+        for (int i = wave; i < 64; i += 4) {   // rows of g: columns of X
+            const int row = r0 + lane, col = c0 + i;
+            tile[lane][i] = row < r && col < c ? (float)(load_value(a.g, base + (int64_t)col * a.ld + row, a.type) * inv) : 0.f;
+        }
+        __syncthreads();
+    }
+    uint16_t* const x = a.x + (int64_t)blockIdx.z * a.planes * a.xsize;
+    for (int i = wave; i < 64; i += 4) {
+        const int row = r0 + i, col = c0 + lane;
+        if (row >= a.rp || col >= a.cp) continue;
+        const float v = a.tall ? tile[i][lane] : (row < r && col < c ? (float)(load_value(a.g, base + (int64_t)row * a.ld + col, a.type) * inv) : 0.f);
+        store_planes(x + (int64_t)row * a.cp + col, a.xsize, a.planes, v);
+    }
+}
+
+// out of a tall matrix: X transposed
+__global__ __launch_bounds__(256) void emit_kernel(MatrixArgs a) {
+    __shared__ float tile[64][65];
+    const int c0 = blockIdx.x * 64, r0 = blockIdx.y * 64;
+    const uint16_t* const x = a.x + (int64_t)blockIdx.z * a.planes * a.xsize;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int i = wave; i < 64; i += 4) {
+        const int row = r0 + i, col = c0 + lane;
+        tile[lane][i] = row < a.rp && col < a.cp ? load_planes(x + (int64_t)row * a.cp + col, a.xsize, a.planes) : 0.f;
+    }
+    __syncthreads();
+    for (int i = wave; i < 64; i += 4) {
+        const int row = c0 + i, col = r0 + lane;   // of g
+        if (row < a.rows && col < a.cols)
+            store_value(a.out, ((int64_t)blockIdx.z * a.rows + row) * a.cols + col, a.type, tile[i][lane] * a.out_scale);
+    }
+}
+
+struct StepArgs {
+    const uint16_t *x, *in;    // X of the step; A (forming B), B (forming X)
+    uint16_t* y;               // A, B or the next X
+    int64_t xsize, asize;
+    int rp, cp, planes;
+    ProductPlanes pairs;
+    int tiles_p, tiles_q, batch;
+    float first, second;       // of what is added, of the product
+    // of the last step of a matrix that is not tall: the result
+    void* out;
+    int rows, cols, type;
+    float out_scale;
+};
+
+// tile t of those on and below the diagonal
+__device__ __forceinline__ void triangle(uint32_t t, int& p, int& q) {
+    int i = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
+    while ((uint32_t)(i + 1) * (i + 2) / 2 <= t) ++i;
+    while ((uint32_t)i * (i + 1) / 2 > t) --i;
+    p = __builtin_amdgcn_readfirstlane(i);   // (uniform, but formed in vector registers)
+    q = __builtin_amdgcn_readfirstlane((int)(t - (uint32_t)i * (i + 1) / 2));
+}
+
+// A = X X^T / scale, or B = first A + second A A^T
+template <class C, bool SQUARE>
+__global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void gram_kernel(StepArgs a) {
+    __shared__ __align__(1024) char smem[C::LDS];
+    const uint32_t each = (uint32_t)a.tiles_p * (a.tiles_p + 1) / 2, total = each * (uint32_t)a.batch, per = (total + 7) / 8;
+    const uint32_t id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if ((blockIdx.x >> 3) >= per || id >= total) return;   // uniform
+    const uint32_t m = (uint32_t)__builtin_amdgcn_readfirstlane((int)(id / each));
+    int tp, tq;
+    triangle(id - m * each, tp, tq);
+    const int p0 = tp * C::BM, q0 = tq * C::BN;
+    const int64_t size = SQUARE ? a.asize : a.xsize;
+    const uint16_t* const src = (SQUARE ? a.in : a.x) + (int64_t)m * a.planes * size;
+    const ProductOperand o = {src, size, SQUARE ? a.rp : a.cp, a.rp, 0};
+    floatx4 acc[C::TM][C::TN];
+    C::run(o, o, a.pairs, p0, q0, 0, (SQUARE ? a.rp : a.cp) / IVFR_PRODUCT_K, smem, acc);
+    uint16_t* const y = a.y + (int64_t)m * a.planes * a.asize;
+#pragma unroll
+    for (int u = 0; u < C::TN; ++u) {
+        const int q = q0 + C::q_of(u);
+        if (q >= a.rp) continue;
+#pragma unroll
+        for (int t = 0; t < C::TM; t += 2) {
+            const int p = p0 + C::p_of(t);
+            if (p >= a.rp) continue;   // (a multiple of 8, as p)
+            float v[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) v[r] = a.second * acc[t + (r >> 2)][u][r & 3];
+            const int64_t at = (int64_t)q * a.rp + p;
+            if constexpr (SQUARE) {
+                const half8v h = *reinterpret_cast<const half8v*>(src + at);
+                half8v l = {0, 0, 0, 0, 0, 0, 0, 0};
+                if (a.planes > 1) l = *reinterpret_cast<const half8v*>(src + a.asize + at);
+#pragma unroll
+                for (int r = 0; r < 8; ++r) v[r] += a.first * ((float)h[r] + (float)l[r]);
+            }
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {   // planes
+                if (n >= a.planes) break;   // uniform
+                uint16_t* const o = y + n * a.asize;
+                short8v h;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    const uint16_t b = to_half(v[r]);
+                    h[r] = (short)b;
+                    v[r] -= from_half(b);
+                    if (tp != tq) o[(int64_t)(p + r) * a.rp + q] = b;
+                }
+                *reinterpret_cast<short8v*>(o + at) = h;
+            }
+        }
+    }
+}
+
+typedef _Float16 half4v __attribute__((ext_vector_type(4)));
+
+// X <- first X + second B X
+template <class C>
+__global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void update_kernel(StepArgs a) {
+    __shared__ __align__(1024) char smem[C::LDS];
+    const ProductTile tile = product_tile(a.tiles_p, a.tiles_q, a.batch);
+    if (!tile.any) return;   // uniform
+    const int p0 = tile.p * C::BM, q0 = tile.q * C::BN;
+    const uint16_t* const x = a.x + (int64_t)tile.split * a.planes * a.xsize;
+    const ProductOperand P = {x, a.xsize, a.cp, a.cp, a.rp}, Q = {a.in + (int64_t)tile.split * a.planes * a.asize, a.asize, a.rp, a.rp, 0};
+    floatx4 acc[C::TM][C::TN];
+    C::run(P, Q, a.pairs, p0, q0, 0, a.rp / IVFR_PRODUCT_K, smem, acc);
+    uint16_t* const y = a.y + (int64_t)tile.split * a.planes * a.xsize;
+#pragma unroll
+    for (int u = 0; u < C::TN; ++u) {
+        const int q = q0 + C::q_of(u);
+        if (q >= a.rp) continue;
+#pragma unroll
+        for (int t = 0; t < C::TM; ++t) {
+            const int p = p0 + C::p_of(t);
+            if (p >= a.cp) continue;   // (a multiple of 4, as p)
+            const int64_t at = (int64_t)q * a.cp + p;
+            const half4v h = *reinterpret_cast<const half4v*>(x + at);
+            half4v l = {0, 0, 0, 0};
+            if (a.planes > 1) l = *reinterpret_cast<const half4v*>(x + a.xsize + at);
+            float v[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = fmaf(a.first, (float)h[r] + (float)l[r], a.second * acc[t][u][r]);
+            if (a.out) {
+                if (q >= a.rows) continue;
+                const int64_t o = ((int64_t)tile.split * a.rows + q) * a.cols + p;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (p + r < a.cols) store_value(a.out, o + r, a.type, v[r] * a.out_scale);
+            } else {
+                half4v n;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) n[r] = (_Float16)v[r];
+                *reinterpret_cast<half4v*>(y + at) = n;
+                if (a.planes > 1) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) n[r] = (_Float16)(v[r] - (float)n[r]);
+                    *reinterpret_cast<half4v*>(y + a.xsize + at) = n;
+                }
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- host
+
+static inline int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+
+static int ortho_check(const ivfr_orthogonalize_args* a) {
+    IVFR_REQUIRE(a, "orthogonalize: null arguments");
+    IVFR_REQUIRE(a->type == IVFR_TYPE_F32 || a->type == IVFR_TYPE_F16 || a->type == IVFR_TYPE_BF16, "orthogonalize: type must be IVFR_TYPE_F32, _F16 or _BF16, got %d", a->type);
+    IVFR_REQUIRE(a->batch >= 0 && a->batch <= 65535 && a->rows >= 1 && a->cols >= 1 && a->rows <= 1 << 20 && a->cols <= 1 << 20,
+                 "orthogonalize: batch must be in [0, 65535], rows and cols in [1, 2^20], got %lld, %d, %d", (long long)a->batch, a->rows, a->cols);
+    IVFR_REQUIRE(std::min(a->rows, a->cols) <= 1 << 16, "orthogonalize: the shorter side must be at most 65536, got %d", std::min(a->rows, a->cols));
+    IVFR_REQUIRE(a->ld >= a->cols && a->batch_stride >= 0 && (a->batch <= 1 || a->batch_stride >= (a->rows - 1) * a->ld + a->cols), "orthogonalize: ld must be at least cols, and matrices must not overlap");
+    IVFR_REQUIRE(a->steps >= 1 && a->steps <= 64 && a->coefficients, "orthogonalize: 1 to 64 steps with coefficients, got %d", a->steps);
+    IVFR_REQUIRE(std::isfinite(a->scale) && a->eps >= 0.f && std::isfinite(a->eps), "orthogonalize: scale must be finite, eps finite and not negative");
+    // what a singular value, at most 1 at first, can become; the numbers of X, A and B are held in fp16 at 2^12, up to 16
+    double top = 1.0;
+    for (int s = 0; s < a->steps; ++s) {
+        const double x = a->coefficients[3 * s], y = a->coefficients[3 * s + 1], z = a->coefficients[3 * s + 2];
+        IVFR_REQUIRE(std::isfinite(x) && std::isfinite(y) && std::isfinite(z), "orthogonalize: the coefficients of step %d must be finite", s);
+        double next = 0.0, b = 0.0;
+        for (int i = 1; i <= 2048; ++i) {
+            const double v = top * i / 2048, w = v * v;
+            next = std::max(next, std::fabs(v * (x + w * (y + w * z))));
+            b = std::max(b, std::fabs(w * (y + w * z)));
+        }
+        next *= 1.005;
+        IVFR_REQUIRE(b < 15.0 && top * top < 15.0 && next < 15.0, "orthogonalize: the coefficients (%g, %g, %g) of step %d take singular values out of range (up to %g)", x, y, z, s, next);
+        top = std::max(next, 1e-3);
+    }
+    return IVFR_OK;
+}
+
+static OrthoPlan ortho_plan(const ivfr_orthogonalize_args& a) {
+    OrthoPlan p = {};
+    p.tall = a.rows > a.cols;
+    p.r = std::min(a.rows, a.cols);
+    p.c = std::max(a.rows, a.cols);
+    p.rp = (int)round_up(p.r, 32);
+    p.cp = (int)round_up(p.c, 32);
+    p.planes = a.type == IVFR_TYPE_F32 ? 2 : 1;
+    p.batch = a.batch;
+    p.xsize = (int64_t)p.rp * p.cp;
+    p.asize = (int64_t)p.rp * p.rp;
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const int64_t here = at;
+        at += round_up(bytes, 256);
+        return here;
+    };
+    p.at_sums = take(p.batch * ORTHO_SUMS * 8);
+    for (int64_t& x : p.at_x) x = take(p.batch * p.planes * p.xsize * 2);
+    p.at_a = take(p.batch * p.planes * p.asize * 2);
+    p.at_b = take(p.batch * p.planes * p.asize * 2);
+    p.bytes = at;
+    return p;
+}
+
+int ivfr_orthogonalize_workspace(const ivfr_orthogonalize_args* args, int64_t* bytes) {
+    IVFR_TRY(ortho_check(args));
+    IVFR_REQUIRE(bytes, "orthogonalize: null output");
+    *bytes = args->batch ? ortho_plan(*args).bytes : 0;
+    return IVFR_OK;
+}
+
+// Tile by the number of them: 256 x 256 where every compute unit gets about one, else the smaller ones.
+static int step_kind(int64_t rows, int64_t cols, int64_t batch, bool triangle) {
+    for (int k = 0; k < 2; ++k) {
+        const int64_t b = k == 0 ? 256 : 128, tp = (rows + b - 1) / b, tq = (cols + b - 1) / b;
+        if ((triangle ? tp * (tp + 1) / 2 : tp * tq) * batch >= (k == 0 ? 200 : 200)) return k;
+    }
+    return 2;
+}
+
+template <class C, bool SQUARE>
+static int launch_gram(StepArgs a, hipStream_t st) {
+    a.tiles_p = (a.rp + C::BM - 1) / C::BM;
+    hipLaunchKernelGGL((gram_kernel<C, SQUARE>), dim3(product_grid((int64_t)a.tiles_p * (a.tiles_p + 1) / 2 * a.batch)), dim3(C::THREADS), 0, st, a);
+    IVFR_HIP(hipGetLastError());
+    return IVFR_OK;
+}
+template <bool SQUARE>
+static int launch_gram_kind(const StepArgs& a, hipStream_t st) {
+    switch (step_kind(a.rp, a.rp, a.batch, true)) {
+        case 0: return launch_gram<Product<256, 256, 2, 4, false, false, true>, SQUARE>(a, st);
+        case 1: return launch_gram<Product<128, 128, 2, 2, false, false, true>, SQUARE>(a, st);
+        default: return launch_gram<Product<64, 64, 2, 2, false, false, true>, SQUARE>(a, st);
+    }
+}
+template <class C>
+static int launch_update(StepArgs a, hipStream_t st) {
+    a.tiles_p = (a.cp + C::BM - 1) / C::BM;
+    a.tiles_q = (a.rp + C::BN - 1) / C::BN;
+    hipLaunchKernelGGL((update_kernel<C>), dim3(product_grid((int64_t)a.tiles_p * a.tiles_q * a.batch)), dim3(C::THREADS), 0, st, a);
+    IVFR_HIP(hipGetLastError());
+    return IVFR_OK;
+}
+
+int ivfr_orthogonalize(const ivfr_orthogonalize_args* args, void* out, void* workspace, int64_t workspace_bytes, void* stream) {
+    IVFR_TRY(ortho_check(args));
+    const ivfr_orthogonalize_args& a = *args;
+    if (a.batch == 0) return IVFR_OK;
+    const OrthoPlan p = ortho_plan(a);
+    const int size = a.type == IVFR_TYPE_F32 ? 4 : 2;
+    IVFR_REQUIRE(a.g && out && workspace, "orthogonalize: null pointer");
+    IVFR_REQUIRE(((uintptr_t)a.g % size) == 0 && ((uintptr_t)out % size) == 0, "orthogonalize: pointers must be aligned to their type");
+    IVFR_REQUIRE(((uintptr_t)workspace & 255) == 0, "orthogonalize: the workspace must be aligned to 256 bytes");
+    IVFR_REQUIRE(workspace_bytes >= p.bytes, "orthogonalize: the workspace has %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)p.bytes);
+    IVFR_HIP(hipSetDevice(a.device));
+    hipStream_t st = (hipStream_t)stream;
+    char* const ws = (char*)workspace;
+    MatrixArgs m = {a.g, a.ld, a.batch_stride, a.rows, a.cols, a.type, p.tall, p.rp, p.cp, p.planes, p.xsize, a.eps,
+                    (double*)(ws + p.at_sums), (uint16_t*)(ws + p.at_x[0]), out, a.scale / ORTHO_SCALE};
+    hipLaunchKernelGGL(squares_kernel, dim3(ORTHO_SUMS, (unsigned)p.batch), dim3(256), 0, st, m);
+    IVFR_HIP(hipGetLastError());
+    const dim3 tiles((unsigned)((p.cp + 63) / 64), (unsigned)((p.rp + 63) / 64), (unsigned)p.batch);
+    hipLaunchKernelGGL(fill_kernel, tiles, dim3(256), 0, st, m);
+    IVFR_HIP(hipGetLastError());
+    StepArgs s = {};
+    s.xsize = p.xsize;
+    s.asize = p.asize;
+    s.rp = p.rp;
+    s.cp = p.cp;
+    s.planes = p.planes;
+    s.pairs = product_planes(p.planes);
+    s.batch = (int)p.batch;
+    s.rows = a.rows;
+    s.cols = a.cols;
+    s.type = a.type;
+    s.out_scale = a.scale / ORTHO_SCALE;
+    for (int i = 0; i < a.steps; ++i) {
+        const float* const k = a.coefficients + 3 * i;
+        s.x = (uint16_t*)(ws + p.at_x[i & 1]);
+        s.y = (uint16_t*)(ws + p.at_a);
+        s.second = 1.f / ORTHO_SCALE;
+        IVFR_TRY(launch_gram_kind<false>(s, st));
+        s.in = s.y;
+        s.y = (uint16_t*)(ws + p.at_b);
+        s.first = k[1];
+        s.second = k[2] / ORTHO_SCALE;
+        IVFR_TRY(launch_gram_kind<true>(s, st));
+        s.in = s.y;
+        s.y = (uint16_t*)(ws + p.at_x[(i + 1) & 1]);
+        s.first = k[0];
+        s.second = 1.f / ORTHO_SCALE;
+        s.out = i + 1 == a.steps && !p.tall ? out : nullptr;
+        switch (step_kind(p.cp, p.rp, p.batch, false)) {
+            case 0: IVFR_TRY((launch_update<Product<256, 256, 2, 4, true, false, true>>(s, st))); break;
+            case 1: IVFR_TRY((launch_update<Product<128, 128, 2, 2, true, false, true>>(s, st))); break;
+            default: IVFR_TRY((launch_update<Product<64, 64, 2, 2, true, false, true>>(s, st))); break;
+        }
+    }
+    if (p.tall) {
+        m.x = (uint16_t*)(ws + p.at_x[a.steps & 1]);
+        hipLaunchKernelGGL(emit_kernel, tiles, dim3(256), 0, st, m);
+        IVFR_HIP(hipGetLastError());
+    }
+    return IVFR_OK;
+}

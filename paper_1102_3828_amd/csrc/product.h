@@ -57,11 +57,13 @@ __device__ __forceinline__ ProductTile product_tile(int tiles_p, int tiles_q, in
     const uint32_t id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
     ProductTile t = {0, 0, 0, (blockIdx.x >> 3) < per && id < total};
     const uint32_t each = (uint32_t)tiles_p * (uint32_t)tiles_q;
-    t.split = (int)(id / each);
-    const uint32_t in = id % each, band = 8u * (uint32_t)tiles_q, b = in / band, first = 8 * b;
+    const uint32_t split = id / each;
+    const uint32_t in = id - split * each, band = 8u * (uint32_t)tiles_q, b = in / band, first = 8 * b;
     const uint32_t high = (uint32_t)tiles_p - first < 8u ? (uint32_t)tiles_p - first : 8u;
-    t.p = (int)(first + (in - b * band) % high);
-    t.q = (int)((in - b * band) / high);
+    // (uniform, but divisions are formed in vector registers, and the addresses made of these have to be in scalar ones)
+    t.split = __builtin_amdgcn_readfirstlane((int)split);
+    t.p = __builtin_amdgcn_readfirstlane((int)(first + (in - b * band) % high));
+    t.q = __builtin_amdgcn_readfirstlane((int)((in - b * band) / high));
     return t;
 }
 inline unsigned product_grid(int64_t tiles) { return (unsigned)((tiles + 7) / 8 * 8); }
