@@ -127,7 +127,6 @@ struct StepArgs {
     uint16_t* y;               // A, B or the next X
     int64_t xsize, asize;
     int rp, cp, planes;
-    ProductPlanes pairs;
     int tiles_p, tiles_q, batch;
     float first, second;       // of what is added, of the product
     // of the last step of a matrix that is not tall: the result
@@ -147,7 +146,7 @@ __device__ __forceinline__ void triangle(uint32_t t, int& p, int& q) {
 
 // A = X X^T / scale, or B = first A + second A A^T
 template <class C, bool SQUARE>
-__global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void gram_kernel(StepArgs a) {
+__global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void gram_kernel(StepArgs a) {
     __shared__ __align__(1024) char smem[C::LDS];
     const uint32_t each = (uint32_t)a.tiles_p * (a.tiles_p + 1) / 2, total = each * (uint32_t)a.batch, per = (total + 7) / 8;
     const uint32_t id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
@@ -160,7 +159,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void gram_ke
     const uint16_t* const src = (SQUARE ? a.in : a.x) + (int64_t)m * a.planes * size;
     const ProductOperand o = {src, size, SQUARE ? a.rp : a.cp, a.rp, 0};
     floatx4 acc[C::TM][C::TN];
-    C::run(o, o, a.pairs, p0, q0, 0, (SQUARE ? a.rp : a.cp) / IVFR_PRODUCT_K, smem, acc);
+    C::run(o, o, p0, q0, 0, (SQUARE ? a.rp : a.cp) / IVFR_PRODUCT_K, smem, acc);
     uint16_t* const y = a.y + (int64_t)m * a.planes * a.asize;
 #pragma unroll
     for (int u = 0; u < C::TN; ++u) {
@@ -182,8 +181,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void gram_ke
                 for (int r = 0; r < 8; ++r) v[r] += a.first * ((float)h[r] + (float)l[r]);
             }
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {   // planes
-                if (n >= a.planes) break;   // uniform
+            for (int n = 0; n < C::PLANES; ++n) {
                 uint16_t* const o = y + n * a.asize;
                 short8v h;
 #pragma unroll
@@ -203,15 +201,15 @@ typedef _Float16 half4v __attribute__((ext_vector_type(4)));
 
 // X <- first X + second B X
 template <class C>
-__global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void update_kernel(StepArgs a) {
+__global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void update_kernel(StepArgs a) {
     __shared__ __align__(1024) char smem[C::LDS];
-    const ProductTile tile = product_tile(a.tiles_p, a.tiles_q, a.batch);
+    const ProductTile tile = product_tile(blockIdx.x, a.tiles_p, a.tiles_q, a.batch);
     if (!tile.any) return;   // uniform
     const int p0 = tile.p * C::BM, q0 = tile.q * C::BN;
     const uint16_t* const x = a.x + (int64_t)tile.split * a.planes * a.xsize;
     const ProductOperand P = {x, a.xsize, a.cp, a.cp, a.rp}, Q = {a.in + (int64_t)tile.split * a.planes * a.asize, a.asize, a.rp, a.rp, 0};
     floatx4 acc[C::TM][C::TN];
-    C::run(P, Q, a.pairs, p0, q0, 0, a.rp / IVFR_PRODUCT_K, smem, acc);
+    C::run(P, Q, p0, q0, 0, a.rp / IVFR_PRODUCT_K, smem, acc);
     uint16_t* const y = a.y + (int64_t)tile.split * a.planes * a.xsize;
 #pragma unroll
     for (int u = 0; u < C::TN; ++u) {
@@ -312,37 +310,65 @@ int ivfr_orthogonalize_workspace(const ivfr_orthogonalize_args* args, int64_t* b
     return IVFR_OK;
 }
 
-// Tile by the number of them: 256 x 256 where every compute unit gets about one, else the smaller ones.
-static int step_kind(int64_t rows, int64_t cols, int64_t batch, bool triangle) {
-    for (int k = 0; k < 2; ++k) {
-        const int64_t b = k == 0 ? 256 : 128, tp = (rows + b - 1) / b, tq = (cols + b - 1) / b;
-        if ((triangle ? tp * (tp + 1) / 2 : tp * tq) * batch >= (k == 0 ? 200 : 200)) return k;
+// Tile by the number of them: the largest that gives every compute unit work.
+static int step_tile(int64_t rows, int64_t cols, int64_t batch, int planes, bool triangle) {
+    for (int k = planes == 1 ? 0 : IVFR_TILE_128x128; k < IVFR_TILE_64x64; ++k) {
+        if (triangle && k == IVFR_TILE_256x128) continue;
+        const int64_t tp = (rows + IVFR_TILE_P[k] - 1) / IVFR_TILE_P[k], tq = (cols + IVFR_TILE_Q[k] - 1) / IVFR_TILE_Q[k];
+        if ((triangle ? tp * (tp + 1) / 2 : tp * tq) * batch >= 200) return k;
     }
-    return 2;
+    return IVFR_TILE_64x64;
 }
 
-template <class C, bool SQUARE>
-static int launch_gram(StepArgs a, hipStream_t st) {
+template <int TILE, int PLANES, bool SQUARE>
+static int launch_gram_tile(StepArgs a, hipStream_t st) {
+    typedef typename ProductOf<TILE, false, false, true, PLANES>::T C;
     a.tiles_p = (a.rp + C::BM - 1) / C::BM;
     hipLaunchKernelGGL((gram_kernel<C, SQUARE>), dim3(product_grid((int64_t)a.tiles_p * (a.tiles_p + 1) / 2 * a.batch)), dim3(C::THREADS), 0, st, a);
     IVFR_HIP(hipGetLastError());
     return IVFR_OK;
 }
-template <bool SQUARE>
-static int launch_gram_kind(const StepArgs& a, hipStream_t st) {
-    switch (step_kind(a.rp, a.rp, a.batch, true)) {
-        case 0: return launch_gram<Product<256, 256, 2, 4, false, false, true>, SQUARE>(a, st);
-        case 1: return launch_gram<Product<128, 128, 2, 2, false, false, true>, SQUARE>(a, st);
-        default: return launch_gram<Product<64, 64, 2, 2, false, false, true>, SQUARE>(a, st);
-    }
+template <int PLANES, bool SQUARE>
+static int launch_gram(const StepArgs& a, hipStream_t st) {
+    const int tile = step_tile(a.rp, a.rp, a.batch, PLANES, true);
+    if constexpr (PLANES == 1)
+        if (tile == IVFR_TILE_256x256) return launch_gram_tile<IVFR_TILE_256x256, 1, SQUARE>(a, st);
+    return tile == IVFR_TILE_128x128 ? launch_gram_tile<IVFR_TILE_128x128, PLANES, SQUARE>(a, st) : launch_gram_tile<IVFR_TILE_64x64, PLANES, SQUARE>(a, st);
 }
-template <class C>
-static int launch_update(StepArgs a, hipStream_t st) {
+template <int TILE, int PLANES>
+static int launch_update_tile(StepArgs a, hipStream_t st) {
+    typedef typename ProductOf<TILE, true, false, true, PLANES>::T C;
     a.tiles_p = (a.cp + C::BM - 1) / C::BM;
     a.tiles_q = (a.rp + C::BN - 1) / C::BN;
     hipLaunchKernelGGL((update_kernel<C>), dim3(product_grid((int64_t)a.tiles_p * a.tiles_q * a.batch)), dim3(C::THREADS), 0, st, a);
     IVFR_HIP(hipGetLastError());
     return IVFR_OK;
+}
+template <int PLANES>
+static int launch_update(const StepArgs& a, hipStream_t st) {
+    const int tile = step_tile(a.cp, a.rp, a.batch, PLANES, false);
+    if constexpr (PLANES == 1) {
+        if (tile == IVFR_TILE_256x256) return launch_update_tile<IVFR_TILE_256x256, 1>(a, st);
+        if (tile == IVFR_TILE_256x128) return launch_update_tile<IVFR_TILE_256x128, 1>(a, st);
+    }
+    return tile == IVFR_TILE_128x128 ? launch_update_tile<IVFR_TILE_128x128, PLANES>(a, st) : launch_update_tile<IVFR_TILE_64x64, PLANES>(a, st);
+}
+// one step: A, B, the next X
+template <int PLANES>
+static int launch_step(StepArgs s, const float* k, uint16_t* a, uint16_t* b, uint16_t* x, hipStream_t st) {
+    s.y = a;
+    s.second = 1.f / ORTHO_SCALE;
+    IVFR_TRY((launch_gram<PLANES, false>(s, st)));
+    s.in = a;
+    s.y = b;
+    s.first = k[1];
+    s.second = k[2] / ORTHO_SCALE;
+    IVFR_TRY((launch_gram<PLANES, true>(s, st)));
+    s.in = b;
+    s.y = x;
+    s.first = k[0];
+    s.second = 1.f / ORTHO_SCALE;
+    return launch_update<PLANES>(s, st);
 }
 
 int ivfr_orthogonalize(const ivfr_orthogonalize_args* args, void* out, void* workspace, int64_t workspace_bytes, void* stream) {
@@ -371,33 +397,17 @@ int ivfr_orthogonalize(const ivfr_orthogonalize_args* args, void* out, void* wor
     s.rp = p.rp;
     s.cp = p.cp;
     s.planes = p.planes;
-    s.pairs = product_planes(p.planes);
     s.batch = (int)p.batch;
     s.rows = a.rows;
     s.cols = a.cols;
     s.type = a.type;
     s.out_scale = a.scale / ORTHO_SCALE;
     for (int i = 0; i < a.steps; ++i) {
-        const float* const k = a.coefficients + 3 * i;
         s.x = (uint16_t*)(ws + p.at_x[i & 1]);
-        s.y = (uint16_t*)(ws + p.at_a);
-        s.second = 1.f / ORTHO_SCALE;
-        IVFR_TRY(launch_gram_kind<false>(s, st));
-        s.in = s.y;
-        s.y = (uint16_t*)(ws + p.at_b);
-        s.first = k[1];
-        s.second = k[2] / ORTHO_SCALE;
-        IVFR_TRY(launch_gram_kind<true>(s, st));
-        s.in = s.y;
-        s.y = (uint16_t*)(ws + p.at_x[(i + 1) & 1]);
-        s.first = k[0];
-        s.second = 1.f / ORTHO_SCALE;
         s.out = i + 1 == a.steps && !p.tall ? out : nullptr;
-        switch (step_kind(p.cp, p.rp, p.batch, false)) {
-            case 0: IVFR_TRY((launch_update<Product<256, 256, 2, 4, true, false, true>>(s, st))); break;
-            case 1: IVFR_TRY((launch_update<Product<128, 128, 2, 2, true, false, true>>(s, st))); break;
-            default: IVFR_TRY((launch_update<Product<64, 64, 2, 2, true, false, true>>(s, st))); break;
-        }
+        uint16_t* const next = (uint16_t*)(ws + p.at_x[(i + 1) & 1]);
+        if (p.planes == 1) IVFR_TRY(launch_step<1>(s, a.coefficients + 3 * i, (uint16_t*)(ws + p.at_a), (uint16_t*)(ws + p.at_b), next, st));
+        else IVFR_TRY(launch_step<2>(s, a.coefficients + 3 * i, (uint16_t*)(ws + p.at_a), (uint16_t*)(ws + p.at_b), next, st));
     }
     if (p.tall) {
         m.x = (uint16_t*)(ws + p.at_x[a.steps & 1]);

@@ -3,10 +3,10 @@
 // D[p][q] = sum_k P(p, k) Q(q, k), fp32 accumulation (v_mfma_f32_16x16x32).  Each operand is held with k innermost ("inner": rows of p,
 // contiguous in k) or with its own index innermost ("outer": rows of k, contiguous in p), so no product needs a transposed copy.
 // Several 16-bit planes carry one fp32 operand (its leading part, what that leaves, what that leaves again); the product is then the sum
-// over pairs of planes, one pair after the other on the same accumulators.
+// over pairs of planes, on the same accumulators.
 //
-// A workgroup owns BM x BN outputs.  Stages of 32 k go straight from memory to LDS, four buffers, so that up to four stages are
-// in flight; one barrier a stage.  The fragments of a stage are read from LDS into registers while the products of the stage before
+// A workgroup owns BM x BN outputs.  Stages of KSUB x 32 k go straight from memory to LDS, STAGES buffers, all of them in flight but
+// the one in use; one barrier a stage.  The fragments of a slice of 32 are read from LDS into registers while the products of the slice before
 // are formed.  16-byte chunks of a row lie permuted in LDS (by the row, as the source addresses choose), so that the lanes that LDS serves
 // together read different banks; outer operands are transposed by the LDS read itself (ds_read_b64_tr_b16).
 //
@@ -22,8 +22,7 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half8v __attribute__((ext_vector_type(8)));
 
-#define IVFR_PRODUCT_K 32        // k of a stage
-#define IVFR_PRODUCT_STAGES 4    // LDS buffers
+#define IVFR_PRODUCT_K 32        // k of a slice: one step of the matrix instruction
 #define IVFR_PRODUCT_CU 256      // compute units that launches are cut for
 
 struct ProductOperand {
@@ -34,28 +33,16 @@ struct ProductOperand {
     int rows;               // outer: rows of k that may be read; beyond them the last one is read again
 };
 
-// Pairs of planes (P, Q), four bits each.  Three planes of bf16 (24 bits of an fp32 value): the six products of which the
-// largest neglected one is 2^-24 of the whole; two of fp16 (22 bits and a sign): without the product of the two rests, 2^-22.  Small ones first.
-struct ProductPlanes {
-    uint32_t p, q;
-    int n;
-};
-inline ProductPlanes product_planes(int planes) {
-    if (planes == 3) return {0x001012u, 0x010210u, 6};   // (2,0) (1,1) (0,2) (1,0) (0,1) (0,0)
-    if (planes == 2) return {0x001u, 0x010u, 3};         // (1,0) (0,1) (0,0)
-    return {0u, 0u, 1};
-}
-
 // What a workgroup computes of a launch's tiles: XCDs take contiguous runs of them (blocks go round the eight XCDs, each with an L2 of its
 // own), and a run walks over patches of eight tiles of p.
 struct ProductTile {
     int p, q, split;
     bool any;
 };
-__device__ __forceinline__ ProductTile product_tile(int tiles_p, int tiles_q, int splits) {
+__device__ __forceinline__ ProductTile product_tile(uint32_t block, int tiles_p, int tiles_q, int splits) {
     const uint32_t total = (uint32_t)tiles_p * (uint32_t)tiles_q * (uint32_t)splits, per = (total + 7) / 8;
-    const uint32_t id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    ProductTile t = {0, 0, 0, (blockIdx.x >> 3) < per && id < total};
+    const uint32_t id = (block & 7) * per + (block >> 3);
+    ProductTile t = {0, 0, 0, (block >> 3) < per && id < total};
     const uint32_t each = (uint32_t)tiles_p * (uint32_t)tiles_q;
     const uint32_t split = id / each;
     const uint32_t in = id - split * each, band = 8u * (uint32_t)tiles_q, b = in / band, first = 8 * b;
@@ -68,23 +55,33 @@ __device__ __forceinline__ ProductTile product_tile(int tiles_p, int tiles_q, in
 }
 inline unsigned product_grid(int64_t tiles) { return (unsigned)((tiles + 7) / 8 * 8); }
 
-template <int BM_, int BN_, int WAVES_M_, int WAVES_N_, bool P_OUTER_, bool Q_OUTER_, bool HALF_>
+// PLANES of fp32 operands: 3 of bf16 (24 bits), of which the six products with a + b <= 2 are formed (what they neglect is 2^-24 of the whole), or 2 of
+// fp16 (22 bits and a sign), three products (2^-22).  All planes of a stage's k are in LDS at once.
+template <int BM_, int BN_, int WAVES_M_, int WAVES_N_, bool P_OUTER_, bool Q_OUTER_, bool HALF_, int PLANES_, int KSUB_, int STAGES_>
 struct Product {
     static constexpr int BM = BM_, BN = BN_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_, WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES;
+    static constexpr int PLANES = PLANES_, KSUB = KSUB_, STAGES = STAGES_;      // slices of 32 k in a stage, LDS buffers
     static constexpr bool P_OUTER = P_OUTER_, Q_OUTER = Q_OUTER_, HALF = HALF_;
     static constexpr int TM = BM / WAVES_M / 16, TN = BN / WAVES_N / 16;
-    static constexpr int KB = 2 * IVFR_PRODUCT_K;                               // bytes of a stage's k
-    static constexpr int STAGE = (BM + BN) * KB;                                // bytes of a buffer
-    static constexpr int LDS = IVFR_PRODUCT_STAGES * STAGE;
-    static constexpr int P_LOADS = BM * KB / 1024, Q_LOADS = BN * KB / 1024;    // of 64 lanes x 16 bytes, a stage
-    // Every wavefront issues the same number of loads, so that one count of those in flight holds for all (with fewer loads than
-    // wavefronts some are issued twice, the same bytes to the same place).
+    static constexpr int KB = 2 * IVFR_PRODUCT_K;                               // bytes of a slice's k
+    static constexpr int P_SLICE = BM * KB, Q_SLICE = BN * KB, SLICE = (P_SLICE + Q_SLICE) * PLANES;
+    static constexpr int STAGE = SLICE * KSUB, LDS = STAGES * STAGE;
+    static constexpr int RESIDENT = 163840 / LDS >= 2 ? 2 : 1;                  // workgroups on a compute unit that registers are kept for
+    static constexpr int WAVES_SIMD = WAVES * RESIDENT / 4 >= 1 ? WAVES * RESIDENT / 4 : 1;
+    static constexpr int P_ROWS = P_SLICE / 1024, Q_ROWS = Q_SLICE / 1024;      // loads of 64 lanes x 16 bytes for one plane of a slice
+    static constexpr int P_LOADS = P_ROWS * PLANES * KSUB, Q_LOADS = Q_ROWS * PLANES * KSUB;
+    // Every wavefront issues the same number of loads, so that one count of those in flight holds for all (what is left over is
+    // issued twice, the same bytes to the same place).
     static constexpr int P_EACH = (P_LOADS + WAVES - 1) / WAVES, Q_EACH = (Q_LOADS + WAVES - 1) / WAVES, EACH = P_EACH + Q_EACH;
-    static_assert(P_LOADS % WAVES == 0 || P_LOADS < WAVES, "");
-    static_assert(Q_LOADS % WAVES == 0 || Q_LOADS < WAVES, "");
+    // different offsets of a wavefront's loads inside a plane
+    static constexpr int P_KINDS = P_ROWS > WAVES ? P_ROWS / WAVES : 1, Q_KINDS = Q_ROWS > WAVES ? Q_ROWS / WAVES : 1;
+    static_assert(P_ROWS % WAVES == 0 || WAVES % P_ROWS == 0, "");
+    static_assert(Q_ROWS % WAVES == 0 || WAVES % Q_ROWS == 0, "");
     static_assert(P_OUTER || TM % 2 == 0, "");
     static_assert(!P_OUTER || BM >= 64, "");
     static_assert(!Q_OUTER || BN >= 64, "");
+    static_assert(EACH * (STAGES - 1) < 64 && LDS <= 163840, "");
+    static_assert(PLANES > 1 || KSUB == 1 || KSUB % 2 == 0, "");
 
     // permutation of the chunks of a row in LDS: inner rows have four of them
     static __device__ __forceinline__ int swz_p(int row) { return ((row >> 1) & 1) | ((row >> 2) & 2); }   // rows 0-3, 8-11 together
@@ -104,7 +101,7 @@ struct Product {
         else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     }
 
-    // byte offset, from the operand's first row or column of this tile and the stage's first k, of what lane `lane` of load `i` brings
+    // byte offset, from the operand's first row or column of this tile and the slice's first k, of what lane `lane` of load `i` of a plane brings
     template <bool OUTER, int SIZE, bool IS_P>
     static __device__ __forceinline__ uint32_t source(int i, int lane, int64_t ld, int extent, int rows_left) {
         if constexpr (!OUTER) {
@@ -119,66 +116,55 @@ struct Product {
         }
     }
 
-    // The accumulators of one tile over the stages [first, first + count) of every pair of planes.  p0, q0: the tile's first p and q, below the
-    // operands' extents.
-    static __device__ __forceinline__ void run(const ProductOperand& P, const ProductOperand& Q, const ProductPlanes& planes, int p0, int q0, int first, int count,
-                                               char* smem, floatx4 (&acc)[TM][TN]) {
+    // The accumulators of one tile over the slices [first, first + count).  p0, q0: the tile's first p and q, below the operands' extents.
+    static __device__ __forceinline__ void run(const ProductOperand& P, const ProductOperand& Q, int p0, int q0, int first, int count, char* smem,
+                                               floatx4 (&acc)[TM][TN]) {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-        const uint16_t* const pb = P.base + (P_OUTER ? (int64_t)p0 : p0 * P.ld) + (int64_t)first * IVFR_PRODUCT_K * (P_OUTER ? P.ld : 1);
-        const uint16_t* const qb = Q.base + (Q_OUTER ? (int64_t)q0 : q0 * Q.ld) + (int64_t)first * IVFR_PRODUCT_K * (Q_OUTER ? Q.ld : 1);
         const int64_t pstep = IVFR_PRODUCT_K * (P_OUTER ? P.ld : 1), qstep = IVFR_PRODUCT_K * (Q_OUTER ? Q.ld : 1);
-        uint32_t po[P_EACH], qo[Q_EACH];
+        const uint16_t* pn = P.base + (P_OUTER ? (int64_t)p0 : p0 * P.ld) + first * pstep;   // of the next stage to load
+        const uint16_t* qn = Q.base + (Q_OUTER ? (int64_t)q0 : q0 * Q.ld) + first * qstep;
+        uint32_t po[P_KINDS], qo[Q_KINDS];
 #pragma unroll
-        for (int i = 0; i < P_EACH; ++i) po[i] = source<P_OUTER, BM, true>((wave + i * WAVES) % P_LOADS, lane, P.ld, P.extent - p0, IVFR_PRODUCT_K);
+        for (int i = 0; i < P_KINDS; ++i) po[i] = source<P_OUTER, BM, true>((wave + i * WAVES) % P_ROWS, lane, P.ld, P.extent - p0, IVFR_PRODUCT_K);
 #pragma unroll
-        for (int i = 0; i < Q_EACH; ++i) qo[i] = source<Q_OUTER, BN, false>((wave + i * WAVES) % Q_LOADS, lane, Q.ld, Q.extent - q0, IVFR_PRODUCT_K);
-        const int total = planes.n * count;
-        int pair = 0, at = 0;   // of the next stage to load
-        const uint16_t *pn = pb + (planes.p & 15) * P.plane, *qn = qb + (planes.q & 15) * Q.plane;
+        for (int i = 0; i < Q_KINDS; ++i) qo[i] = source<Q_OUTER, BN, false>((wave + i * WAVES) % Q_ROWS, lane, Q.ld, Q.extent - q0, IVFR_PRODUCT_K);
+        const int stages = (count + KSUB - 1) / KSUB;
+        int at = 0;   // first slice of the next stage to load
         auto load = [&](int buf) {
-            const uint32_t lp = lds0 + buf * STAGE, lq = lp + BM * KB;
-            const int pl = P_OUTER ? P.rows - (first + at) * IVFR_PRODUCT_K : IVFR_PRODUCT_K, ql = Q_OUTER ? Q.rows - (first + at) * IVFR_PRODUCT_K : IVFR_PRODUCT_K;
+            const uint32_t base = lds0 + buf * STAGE;
 #pragma unroll
             for (int i = 0; i < P_EACH; ++i) {
-                const int f = (wave + i * WAVES) % P_LOADS;
-                load16(lp + 1024 * f, P_OUTER && pl < IVFR_PRODUCT_K ? source<P_OUTER, BM, true>(f, lane, P.ld, P.extent - p0, pl) : po[i], pn);
+                const int f = (wave + i * WAVES) % P_LOADS, row = f % P_ROWS, plane = f / P_ROWS % PLANES, sub = f / (P_ROWS * PLANES);
+                const int slice = KSUB == 1 || at + sub < count ? sub : count - 1 - at;   // (past the last one: that again)
+                const int left = P_OUTER ? P.rows - (first + at + slice) * IVFR_PRODUCT_K : IVFR_PRODUCT_K;
+                load16(base + sub * SLICE + plane * P_SLICE + 1024 * row,
+                       P_OUTER && left < IVFR_PRODUCT_K ? source<P_OUTER, BM, true>(row, lane, P.ld, P.extent - p0, left) : po[i % P_KINDS],
+                       pn + slice * pstep + (PLANES > 1 ? plane * P.plane : 0));
             }
 #pragma unroll
             for (int i = 0; i < Q_EACH; ++i) {
-                const int f = (wave + i * WAVES) % Q_LOADS;
-                load16(lq + 1024 * f, Q_OUTER && ql < IVFR_PRODUCT_K ? source<Q_OUTER, BN, false>(f, lane, Q.ld, Q.extent - q0, ql) : qo[i], qn);
+                const int f = (wave + i * WAVES) % Q_LOADS, row = f % Q_ROWS, plane = f / Q_ROWS % PLANES, sub = f / (Q_ROWS * PLANES);
+                const int slice = KSUB == 1 || at + sub < count ? sub : count - 1 - at;
+                const int left = Q_OUTER ? Q.rows - (first + at + slice) * IVFR_PRODUCT_K : IVFR_PRODUCT_K;
+                load16(base + sub * SLICE + PLANES * P_SLICE + plane * Q_SLICE + 1024 * row,
+                       Q_OUTER && left < IVFR_PRODUCT_K ? source<Q_OUTER, BN, false>(row, lane, Q.ld, Q.extent - q0, left) : qo[i % Q_KINDS],
+                       qn + slice * qstep + (PLANES > 1 ? plane * Q.plane : 0));
             }
-            if (++at < count) {
-                pn += pstep;
-                qn += qstep;
-            } else {
-                at = 0;
-                ++pair;
-                pn = pb + ((planes.p >> (4 * pair)) & 15) * P.plane;
-                qn = qb + ((planes.q >> (4 * pair)) & 15) * Q.plane;
-            }
+            at += KSUB;
+            pn += KSUB * pstep;
+            qn += KSUB * qstep;
         };
         const int wm = wave / WAVES_N * (BM / WAVES_M), wn = wave % WAVES_N * (BN / WAVES_N);
         const int r = lane & 15, g = lane >> 4;
         // where this lane's fragments of the first tile lie; the others at constant distances (the permutations repeat every 16 or 32 rows)
-        uint32_t pf[P_OUTER ? 2 : 2], qf[2];
-        if constexpr (P_OUTER) {
+        uint32_t pf[2], qf[2];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) pf[j] = (8 * g + 4 * j + (r >> 2)) * (2 * BM);   // the row of k; the column's chunk comes with the tile
-        } else {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int row = wm + 8 * (r >> 2) + 4 * j + (r & 3);
-                pf[j] = row * KB + 16 * (g ^ swz_p(row));
-            }
-        }
-        if constexpr (Q_OUTER) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) qf[j] = (8 * g + 4 * j + (r >> 2)) * (2 * BN);
-        } else {
-            const int row = wn + r;
-            qf[0] = qf[1] = row * KB + 16 * (g ^ swz_q(row));
+        for (int j = 0; j < 2; ++j) {
+            // outer: the row of k (the column's chunk comes with the tile)
+            const int row = wm + 8 * (r >> 2) + 4 * j + (r & 3), k = 8 * g + 4 * j + (r >> 2);
+            pf[j] = P_OUTER ? k * (2 * BM) : row * KB + 16 * (g ^ swz_p(row));
+            qf[j] = Q_OUTER ? k * (2 * BN) : (wn + r) * KB + 16 * (g ^ swz_q(wn + r));
         }
         auto outer_read = [&](const char* b, const uint32_t (&rows)[2], int column) {   // eight k of column + (l & 15)
             short8v v;
@@ -190,9 +176,9 @@ struct Product {
             }
             return v;
         };
-        auto read = [&](int buf, short8v (&fp)[TM], short8v (&fq)[TN]) {
-            const char* bp = smem + buf * STAGE;
-            const char* bq = bp + BM * KB;
+        auto read = [&](const char* slice, int plane, short8v (&fp)[TM], short8v (&fq)[TN]) {
+            const char* bp = slice + plane * P_SLICE;
+            const char* bq = slice + PLANES * P_SLICE + plane * Q_SLICE;
 #pragma unroll
             for (int t = 0; t < TN; ++t) {
                 if constexpr (Q_OUTER) fq[t] = outer_read(bq, qf, wn + 16 * t);
@@ -204,33 +190,71 @@ struct Product {
                 else fp[t] = *reinterpret_cast<const short8v*>(bp + pf[t & 1] + (t >> 1) * 32 * KB);
             }
         };
+        auto products = [&](const short8v (&fp)[TM], const short8v (&fq)[TN]) {
+#pragma unroll
+            for (int a = 0; a < TM; ++a)
+#pragma unroll
+                for (int b = 0; b < TN; ++b) acc[a][b] = mfma(fp[a], fq[b], acc[a][b]);
+        };
 #pragma unroll
         for (int a = 0; a < TM; ++a)
 #pragma unroll
             for (int b = 0; b < TN; ++b) acc[a][b] = floatx4{0.f, 0.f, 0.f, 0.f};
-        short8v fp[2][TM], fq[2][TN];
+        if (count <= 0) return;   // uniform
 #pragma unroll
-        for (int s = 0; s < IVFR_PRODUCT_STAGES; ++s)
-            if (s < total) load(s);
-        if (total >= IVFR_PRODUCT_STAGES) wait_and_meet<3 * EACH>();
-        else wait_and_meet<0>();
-        if (total > 0) read(0, fp[0], fq[0]);
-        auto step = [&](int s, short8v (&cp)[TM], short8v (&cq)[TN], short8v (&np)[TM], short8v (&nq)[TN]) {
-            if (s + 1 < total) {
-                // in flight: stages up to s + 3; s + 1 is needed, and buffer s & 3 is free once all have read stage s
-                if (s + 3 < total) wait_and_meet<2 * EACH>();
-                else wait_and_meet<0>();
-                if (s + 4 < total) load(s & 3);
-                read((s + 1) & 3, np, nq);
+        for (int s = 0; s < STAGES; ++s)
+            if (s < stages) load(s);
+        int buf = 0;   // of the stage that is being used
+        if constexpr (PLANES == 1) {
+            if (stages >= STAGES) wait_and_meet<(STAGES - 1) * EACH>();
+            else wait_and_meet<0>();
+            short8v fp[2][TM], fq[2][TN];
+            read(smem, 0, fp[0], fq[0]);
+            // slice `sub` of stage s; its fragments are in `c`, those of the next slice go to `n`
+            auto step = [&](int s, int sub, short8v (&cp)[TM], short8v (&cq)[TN], short8v (&np)[TM], short8v (&nq)[TN]) {
+                if (s * KSUB + sub + 1 < count) {
+                    if (sub + 1 < KSUB) read(smem + buf * STAGE + (sub + 1) * SLICE, 0, np, nq);
+                    else {
+                        // loaded are the stages up to s + STAGES - 1; s + 1 is needed, and the buffer of s is free once all have read it
+                        if (s + STAGES - 1 < stages) wait_and_meet<(STAGES - 2) * EACH>();
+                        else wait_and_meet<0>();
+                        if (s + STAGES < stages) load(buf);
+                        buf = buf + 1 == STAGES ? 0 : buf + 1;
+                        read(smem + buf * STAGE, 0, np, nq);
+                    }
+                }
+                products(cp, cq);
+            };
+            if constexpr (KSUB == 1) {
+                for (int s = 0; s < stages; s += 2) {
+                    step(s, 0, fp[0], fq[0], fp[1], fq[1]);
+                    if (s + 1 < stages) step(s + 1, 0, fp[1], fq[1], fp[0], fq[0]);
+                }
+            } else {
+                for (int s = 0; s < stages; ++s)
+#pragma unroll
+                    for (int sub = 0; sub < KSUB; ++sub)
+                        if (s * KSUB + sub < count) step(s, sub, fp[sub & 1], fq[sub & 1], fp[(sub + 1) & 1], fq[(sub + 1) & 1]);
             }
+        } else {
+            for (int s = 0; s < stages; ++s) {
+                // loaded are the stages up to s + STAGES - 2 (the first time one more)
+                if (s + STAGES - 2 < stages) wait_and_meet<(STAGES - 2) * EACH>();
+                else wait_and_meet<0>();
+                if (s > 0 && s - 1 + STAGES < stages) load(buf == 0 ? STAGES - 1 : buf - 1);   // (all have read stage s - 1)
 #pragma unroll
-            for (int a = 0; a < TM; ++a)
+                for (int sub = 0; sub < KSUB; ++sub) {
+                    if (KSUB > 1 && s * KSUB + sub >= count) break;   // uniform
+                    short8v fp[PLANES][TM], fq[PLANES][TN];
 #pragma unroll
-                for (int b = 0; b < TN; ++b) acc[a][b] = mfma(cp[a], cq[b], acc[a][b]);
-        };
-        for (int s = 0; s < total; s += 2) {
-            step(s, fp[0], fq[0], fp[1], fq[1]);
-            if (s + 1 < total) step(s + 1, fp[1], fq[1], fp[0], fq[0]);
+                    for (int n = PLANES - 1; n >= 0; --n) read(smem + buf * STAGE + sub * SLICE, n, fp[n], fq[n]);
+#pragma unroll
+                    for (int sum = PLANES - 1; sum >= 0; --sum)   // small products first
+#pragma unroll
+                        for (int n = 0; n <= sum; ++n) products(fp[n], fq[sum - n]);
+                }
+                buf = buf + 1 == STAGES ? 0 : buf + 1;
+            }
         }
     }
 
@@ -245,41 +269,58 @@ struct Product {
     }
 };
 
+// The tiles that there are.  256 x 256 reads least from LDS and memory; of 256 x 128 (and the smaller ones) a compute unit holds two workgroups, so
+// that one forms products while the other starts or ends a tile; the smaller ones are for fewer outputs, the narrow ones for few rows.
+#define IVFR_TILE_256x256 0
+#define IVFR_TILE_256x128 1
+#define IVFR_TILE_128x128 2
+#define IVFR_TILE_64x64 3
+#define IVFR_TILE_256x64 4
+#define IVFR_TILE_256x16 5
+#define IVFR_TILES 6
+static const int IVFR_TILE_P[IVFR_TILES] = {256, 256, 128, 64, 256, 256}, IVFR_TILE_Q[IVFR_TILES] = {256, 128, 128, 64, 64, 16};
+template <int TILE, bool PO, bool QO, bool HALF, int PLANES> struct ProductOf;
+template <bool PO, bool QO, bool HALF> struct ProductOf<0, PO, QO, HALF, 1> { typedef Product<256, 256, 2, 4, PO, QO, HALF, 1, 1, 4> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<1, PO, QO, HALF, 1> { typedef Product<256, 128, 2, 2, PO, QO, HALF, 1, 1, 3> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<2, PO, QO, HALF, 1> { typedef Product<128, 128, 2, 2, PO, QO, HALF, 1, 1, 4> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<3, PO, QO, HALF, 1> { typedef Product<64, 64, 2, 2, PO, QO, HALF, 1, 2, 4> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<4, PO, QO, HALF, 1> { typedef Product<256, 64, 8, 1, PO, QO, HALF, 1, 1, 4> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<5, PO, QO, HALF, 1> { typedef Product<256, 16, 8, 1, PO, QO, HALF, 1, 1, 4> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<2, PO, QO, HALF, 2> { typedef Product<128, 128, 2, 4, PO, QO, HALF, 2, 1, 4> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<3, PO, QO, HALF, 2> { typedef Product<64, 64, 2, 2, PO, QO, HALF, 2, 1, 4> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<2, PO, QO, HALF, 3> { typedef Product<128, 128, 2, 4, PO, QO, HALF, 3, 1, 3> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<3, PO, QO, HALF, 3> { typedef Product<64, 64, 2, 2, PO, QO, HALF, 3, 1, 3> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<4, PO, QO, HALF, 3> { typedef Product<256, 64, 8, 1, PO, QO, HALF, 3, 1, 2> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<5, PO, QO, HALF, 3> { typedef Product<256, 16, 8, 1, PO, QO, HALF, 3, 1, 3> T; };
+
 // rounding to nearest, ties to even
 __device__ __forceinline__ uint16_t to_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 __device__ __forceinline__ float from_bf16(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 __device__ __forceinline__ uint16_t to_half(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
 __device__ __forceinline__ float from_half(uint16_t x) { return (float)__builtin_bit_cast(_Float16, x); }
 
-// ---- products that are stored, in fp32 sums over parts of k where there are few tiles (product.hip)
+// ---- products that are stored, as fp32 sums over parts of k where there are few tiles (product.hip)
 
-#define IVFR_OUT_F32 0
-#define IVFR_OUT_F16 1
-#define IVFR_OUT_BF16 2
-
-// out[q][p] = alpha * unit * sum_k P(p, k) Q(q, k) for p < np, q < nq
-struct ProductOut {
+// values: IVFR_TYPE_*
+struct ProductOut {            // out[q][p] = alpha * unit * sum_k P(p, k) Q(q, k) for p < np, q < nq
     ProductOperand P, Q;       // P outer
-    bool q_outer, half;
-    ProductPlanes planes;
-    int stages;                // of 32 k
+    int planes;
+    int slices;                // of 32 k
     int np, nq;
-    int type;                  // IVFR_OUT_*
+    int type;
     float alpha;
-    const float* unit;         // device factor, or null
+    const float* unit;         // unit[1] is a device factor, or null
     void* out;
     int64_t ld;
-    // sums over parts of k: slots slot0 .. slot0 + splits - 1 of partial [slot][nq][np_pad] are written instead of out
+    // sums over parts of k: slots slot0 .. of partial [slot][nq][np_pad] are written instead of out
     float* partial;
     int slot0;
+    int tile, splits;          // how it is cut (product_cut)
 };
-// how such a product is cut
-struct ProductPlan {
-    int kind, splits;          // tile, parts of k
-};
-ProductPlan product_plan(int64_t np, int64_t nq, int64_t stages, int pairs, bool q_outer, int n_cu);
+// The tile and the number of parts of k for a product of these sizes; q_outer: Q too.
+void product_cut(int64_t np, int64_t nq, int64_t slices, int planes, bool q_outer, int* tile, int* splits);
 inline int64_t product_pad(int64_t np) { return (np + 3) / 4 * 4; }
-// partial == null: plan.splits must be 1
-int product_launch(const ProductOut& a, const ProductPlan& plan, hipStream_t st);
-// out[q][p] = alpha * unit * sum over the slots, in their order
-int product_join(const float* partial, int slots, int64_t nq, int np, int type, float alpha, const float* unit, void* out, int64_t ld, hipStream_t st);
+// x: Q inner; w: Q outer.  Both in one launch where their tiles are the same small ones.
+int product_launch(const ProductOut& x, const ProductOut& w, bool half, hipStream_t st);
+// out[q][p] = alpha * unit * sum over `slots` slots of o.partial, in their order; up to two of them in one launch (slots 0: none)
+int product_join(const ProductOut& a, int a_slots, const ProductOut& b, int b_slots, hipStream_t st);

@@ -1,26 +1,21 @@
-// Products that are stored (product.h): gradients of softmax.hip.
+// Products that are stored (product.h): the gradients of softmax.hip.
 #include "product.h"
 
 #include <algorithm>
 
-struct OutArgs {
-    ProductOut o;
-    int tiles_p, tiles_q, splits, per;   // stages of a part
-};
-
 __device__ __forceinline__ void store_value(void* out, int64_t at, int type, float x) {
-    if (type == IVFR_OUT_F32) ((float*)out)[at] = x;
-    else ((uint16_t*)out)[at] = type == IVFR_OUT_F16 ? to_half(x) : to_bf16(x);
+    if (type == IVFR_TYPE_F32) ((float*)out)[at] = x;
+    else ((uint16_t*)out)[at] = type == IVFR_TYPE_F16 ? to_half(x) : to_bf16(x);
 }
 
 // four consecutive values, the first `some` of them in range
 __device__ __forceinline__ void store_four(void* out, int64_t at, int type, const floatx4 x, int some, bool whole) {
     if (whole && some >= 4) {
-        if (type == IVFR_OUT_F32) *reinterpret_cast<floatx4*>((float*)out + at) = x;
+        if (type == IVFR_TYPE_F32) *reinterpret_cast<floatx4*>((float*)out + at) = x;
         else {
             short4v h;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) h[r] = (short)(type == IVFR_OUT_F16 ? to_half(x[r]) : to_bf16(x[r]));
+            for (int r = 0; r < 4; ++r) h[r] = (short)(type == IVFR_TYPE_F16 ? to_half(x[r]) : to_bf16(x[r]));
             *reinterpret_cast<short4v*>((uint16_t*)out + at) = h;
         }
     } else {
@@ -31,18 +26,16 @@ __device__ __forceinline__ void store_four(void* out, int64_t at, int type, cons
 }
 
 template <class C>
-__global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void out_kernel(OutArgs a) {
-    __shared__ __align__(1024) char smem[C::LDS];
-    const ProductTile tile = product_tile(a.tiles_p, a.tiles_q, a.splits);
+__device__ __forceinline__ void form(const ProductOut& o, uint32_t block, char* smem) {
+    const ProductTile tile = product_tile(block, (o.np + C::BM - 1) / C::BM, (o.nq + C::BN - 1) / C::BN, o.splits);
     if (!tile.any) return;   // uniform
-    const ProductOut& o = a.o;
-    const int p0 = tile.p * C::BM, q0 = tile.q * C::BN, first = tile.split * a.per;
-    const int count = o.stages - first < a.per ? o.stages - first : a.per;
+    const int per = (o.slices + o.splits - 1) / o.splits;
+    const int p0 = tile.p * C::BM, q0 = tile.q * C::BN, first = tile.split * per;
     floatx4 acc[C::TM][C::TN];
-    C::run(o.P, o.Q, o.planes, p0, q0, first, count, smem, acc);
+    C::run(o.P, o.Q, p0, q0, first, o.slices - first < per ? o.slices - first : per, smem, acc);
     const float alpha = o.partial ? 1.f : o.alpha * (o.unit ? o.unit[1] : 1.f);
     const int64_t ld = o.partial ? (o.np + 3) / 4 * 4 : o.ld;
-    const int type = o.partial ? IVFR_OUT_F32 : o.type, limit = o.partial ? (int)ld : o.np;
+    const int type = o.partial ? IVFR_TYPE_F32 : o.type, limit = o.partial ? (int)ld : o.np;
     void* const out = o.partial ? (void*)(o.partial + (int64_t)(o.slot0 + tile.split) * o.nq * ld) : o.out;
     const bool whole = ld % 4 == 0 && ((uintptr_t)out & 15) == 0;   // uniform
 #pragma unroll
@@ -57,79 +50,126 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void out_ker
     }
 }
 
-// A thread takes four neighbouring values through all slots.
-__global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ partial, int slots, int64_t nq, int np, int type, float alpha,
-                                                   const float* __restrict__ unit, void* __restrict__ out, int64_t ld) {
-    const int pad = (np + 3) / 4 * 4, quads = pad / 4;
-    const int64_t total = nq * quads, slot = nq * pad;
-    const float f = alpha * (unit ? unit[1] : 1.f);
-    const bool whole = ld % 4 == 0 && ((uintptr_t)out & 15) == 0;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t q = i / quads;
-        const int p = (int)(i - q * quads) * 4;
-        const float* s = partial + 4 * i;
-        floatx4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-        for (int k = 0; k < slots; ++k) sum += *reinterpret_cast<const floatx4*>(s + k * slot);
-        store_four(out, q * ld + p, type, sum * f, np - p, whole);
-    }
+template <class C>
+__global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void out_kernel(ProductOut o) {
+    __shared__ __align__(1024) char smem[C::LDS];
+    form<C>(o, blockIdx.x, smem);
+}
+// The first `blocks` workgroups form x, the others w.
+template <class CX, class CW>
+__global__ __launch_bounds__(CX::THREADS, CX::WAVES_SIMD) void two_out_kernel(ProductOut x, ProductOut w, uint32_t blocks) {
+    __shared__ __align__(1024) char smem[CX::LDS > CW::LDS ? CX::LDS : CW::LDS];
+    if (blockIdx.x < blocks) form<CX>(x, blockIdx.x, smem);
+    else form<CW>(w, blockIdx.x - blocks, smem);
 }
 
-int product_join(const float* partial, int slots, int64_t nq, int np, int type, float alpha, const float* unit, void* out, int64_t ld, hipStream_t st) {
-    const int64_t total = nq * (product_pad(np) / 4);
-    hipLaunchKernelGGL(join_kernel, dim3((unsigned)std::min<int64_t>((total + 255) / 256, 8192)), dim3(256), 0, st, partial, slots, nq, np, type, alpha, unit, out, ld);
+// A thread takes four neighbouring values through all slots.
+__device__ __forceinline__ void join(const ProductOut& o, int slots, int64_t block, int64_t blocks) {
+    const int pad = (o.np + 3) / 4 * 4, quads = pad / 4;
+    const int64_t total = (int64_t)o.nq * quads, slot = (int64_t)o.nq * pad;
+    const float f = o.alpha * (o.unit ? o.unit[1] : 1.f);
+    const bool whole = o.ld % 4 == 0 && ((uintptr_t)o.out & 15) == 0;
+    for (int64_t i = block * 256 + threadIdx.x; i < total; i += blocks * 256) {
+        const int64_t q = i / quads;
+        const int p = (int)(i - q * quads) * 4;
+        const float* s = o.partial + 4 * i;
+        floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+        for (int k = 0; k < slots; ++k) sum += *reinterpret_cast<const floatx4*>(s + k * slot);
+        store_four(o.out, q * o.ld + p, o.type, sum * f, o.np - p, whole);
+    }
+}
+__global__ __launch_bounds__(256) void join_kernel(ProductOut a, int a_slots, uint32_t a_blocks, ProductOut b, int b_slots) {
+    if (blockIdx.x < a_blocks) join(a, a_slots, blockIdx.x, a_blocks);
+    else join(b, b_slots, blockIdx.x - a_blocks, gridDim.x - a_blocks);
+}
+static unsigned join_blocks(const ProductOut& o) { return (unsigned)std::min<int64_t>(((int64_t)o.nq * (product_pad(o.np) / 4) + 255) / 256, 4096); }
+
+int product_join(const ProductOut& a, int a_slots, const ProductOut& b, int b_slots, hipStream_t st) {
+    const unsigned ab = a_slots ? join_blocks(a) : 0, bb = b_slots ? join_blocks(b) : 0;
+    if (ab + bb == 0) return IVFR_OK;
+    hipLaunchKernelGGL(join_kernel, dim3(ab + bb), dim3(256), 0, st, a, a_slots, ab, b, b_slots);
     IVFR_HIP(hipGetLastError());
     return IVFR_OK;
 }
 
-// Tiles of p x q; workgroups that a compute unit holds (by LDS); cycles of a stage on a compute unit that holds that many, by what was measured
-struct Kind {
-    int bm, bn, resident;
-    double stage;
+// Cycles of a slice on a compute unit that holds as many workgroups as it can, and that number, by what was measured; planes 1, 2, 3
+struct TileCost {
+    int resident[3];
+    double slice[3];
 };
-static const Kind KINDS[] = {{256, 256, 1, 1300}, {128, 128, 2, 900}, {64, 64, 5, 900}, {256, 16, 2, 420}};
+static const TileCost COSTS[IVFR_TILES] = {{{1, 0, 0}, {1600, 0, 0}}, {{2, 0, 0}, {1700, 0, 0}}, {{2, 1, 1}, {1000, 1500, 2600}},
+                                           {{2, 2, 2}, {320, 700, 1200}}, {{0, 0, 0}, {0, 0, 0}}, {{2, 0, 1}, {420, 0, 900}}};
 
-ProductPlan product_plan(int64_t np, int64_t nq, int64_t stages, int pairs, bool q_outer, int n_cu) {
-    ProductPlan best = {0, 1};
+void product_cut(int64_t np, int64_t nq, int64_t slices, int planes, bool q_outer, int* tile, int* splits) {
     double least = 1e300;
-    for (int k = 0; k < 4; ++k) {
-        if (k == 3 && (q_outer || nq > 64)) continue;
-        const int64_t tiles = ((np + KINDS[k].bm - 1) / KINDS[k].bm) * ((nq + KINDS[k].bn - 1) / KINDS[k].bn);
-        for (int s = 1; s <= 128 && s <= stages; s *= 2) {
-            const int64_t per = (stages + s - 1) / s, parts = (stages + per - 1) / per, slots = (int64_t)n_cu * KINDS[k].resident;
+    for (int k = 0; k < IVFR_TILES; ++k) {
+        const int resident = COSTS[k].resident[planes - 1];
+        if (!resident || (k == IVFR_TILE_256x16 && (q_outer || nq > 64)) || (k == IVFR_TILE_256x128 && q_outer)) continue;   // (256 x 128 with both outer: out of registers)
+        const int64_t tiles = ((np + IVFR_TILE_P[k] - 1) / IVFR_TILE_P[k]) * ((nq + IVFR_TILE_Q[k] - 1) / IVFR_TILE_Q[k]);
+        for (int s = 1; s <= 128 && s <= slices; s *= 2) {
+            const int64_t per = (slices + s - 1) / s, parts = (slices + per - 1) / per, slots = (int64_t)IVFR_PRODUCT_CU * resident;
             const double rounds = (double)((tiles * parts + slots - 1) / slots);
-            double cost = rounds * ((double)per * pairs * KINDS[k].stage + 4000.0);
+            // (workgroups that share a compute unit share its matrix units)
+            const double share = tiles * parts <= IVFR_PRODUCT_CU ? 0.6 : 1.0;
+            double cost = rounds * ((double)per * COSTS[k].slice[planes - 1] * share + 5000.0);
             if (s > 1) cost += 6000.0 + (double)parts * np * nq * 8.0 / 1900.0;   // partial sums written and read, a launch
             if (cost < least) {
                 least = cost;
-                best = {k, (int)parts};
+                *tile = k;
+                *splits = (int)parts;
             }
         }
     }
-    return best;
 }
 
-template <class C>
-static int launch(const ProductOut& o, int splits, hipStream_t st) {
-    OutArgs a = {o, (o.np + C::BM - 1) / C::BM, (o.nq + C::BN - 1) / C::BN, splits, (o.stages + splits - 1) / splits};
-    hipLaunchKernelGGL((out_kernel<C>), dim3(product_grid((int64_t)a.tiles_p * a.tiles_q * splits)), dim3(C::THREADS), 0, st, a);
+static unsigned out_blocks(const ProductOut& o) {
+    return product_grid((int64_t)((o.np + IVFR_TILE_P[o.tile] - 1) / IVFR_TILE_P[o.tile]) * ((o.nq + IVFR_TILE_Q[o.tile] - 1) / IVFR_TILE_Q[o.tile]) * o.splits);
+}
+
+template <int TILE, bool QO, bool HALF, int PLANES>
+static int launch_one(const ProductOut& o, hipStream_t st) {
+    typedef typename ProductOf<TILE, true, QO, HALF, PLANES>::T C;
+    hipLaunchKernelGGL((out_kernel<C>), dim3(out_blocks(o)), dim3(C::THREADS), 0, st, o);
     IVFR_HIP(hipGetLastError());
     return IVFR_OK;
 }
-
-template <bool HALF>
-static int launch_kind(const ProductOut& o, const ProductPlan& plan, hipStream_t st) {
-    if (o.q_outer) {
-        if (plan.kind == 0) return launch<Product<256, 256, 2, 4, true, true, HALF>>(o, plan.splits, st);
-        if (plan.kind == 1) return launch<Product<128, 128, 2, 2, true, true, HALF>>(o, plan.splits, st);
-        return launch<Product<64, 64, 2, 2, true, true, HALF>>(o, plan.splits, st);
+template <bool QO, bool HALF, int PLANES>
+static int launch_tile(const ProductOut& o, hipStream_t st) {
+    switch (o.tile) {
+        case 2: return launch_one<2, QO, HALF, PLANES>(o, st);
+        case 3: return launch_one<3, QO, HALF, PLANES>(o, st);
+        case 5:
+            if constexpr (!QO) return launch_one<5, false, HALF, PLANES>(o, st);
+            break;
+        case 0:
+            if constexpr (PLANES == 1) return launch_one<0, QO, HALF, 1>(o, st);
+            break;
+        case 1:
+            if constexpr (PLANES == 1 && !QO) return launch_one<1, false, HALF, 1>(o, st);
+            break;
     }
-    if (plan.kind == 0) return launch<Product<256, 256, 2, 4, true, false, HALF>>(o, plan.splits, st);
-    if (plan.kind == 1) return launch<Product<128, 128, 2, 2, true, false, HALF>>(o, plan.splits, st);
-    if (plan.kind == 2) return launch<Product<64, 64, 2, 2, true, false, HALF>>(o, plan.splits, st);
-    return launch<Product<256, 16, 8, 1, true, false, HALF>>(o, plan.splits, st);
+    ivfr_set_error("no such tile of a product: %d", o.tile);
+    return IVFR_ERR_INVALID_ARG;
+}
+template <int TILE, bool HALF, int PLANES>
+static int launch_two(const ProductOut& x, const ProductOut& w, hipStream_t st) {
+    typedef typename ProductOf<TILE, true, false, HALF, PLANES>::T CX;
+    typedef typename ProductOf<TILE, true, true, HALF, PLANES>::T CW;
+    const unsigned blocks = out_blocks(x);
+    hipLaunchKernelGGL((two_out_kernel<CX, CW>), dim3(blocks + out_blocks(w)), dim3(CX::THREADS), 0, st, x, w, blocks);
+    IVFR_HIP(hipGetLastError());
+    return IVFR_OK;
+}
+template <bool HALF, int PLANES>
+static int launch_both(const ProductOut& x, const ProductOut& w, hipStream_t st) {
+    if (x.tile == w.tile && x.tile == IVFR_TILE_128x128) return launch_two<2, HALF, PLANES>(x, w, st);
+    if (x.tile == w.tile && x.tile == IVFR_TILE_64x64) return launch_two<3, HALF, PLANES>(x, w, st);
+    IVFR_TRY((launch_tile<false, HALF, PLANES>(x, st)));
+    return launch_tile<true, HALF, PLANES>(w, st);
 }
 
-int product_launch(const ProductOut& o, const ProductPlan& plan, hipStream_t st) {
-    return o.half ? launch_kind<true>(o, plan, st) : launch_kind<false>(o, plan, st);
+int product_launch(const ProductOut& x, const ProductOut& w, bool half, hipStream_t st) {
+    if (x.planes == 3) return launch_both<false, 3>(x, w, st);
+    return half ? launch_both<true, 1>(x, w, st) : launch_both<false, 1>(x, w, st);
 }

@@ -21,16 +21,25 @@
 struct PackArgs {
     const void* src;
     int64_t ld, rows, rows_out, ld_out;
-    int d, planes, vec;        // vec: rows start at 16-byte boundaries
+    int d, vec;                // vec: rows start at 16-byte boundaries
     uint16_t* dst;
     const float* offset;       // [rows] or null
     const int64_t* targets;    // [rows] or null
+    unsigned blocks;           // of the launch that work on it
+};
+// fp16 calls: e is written in a unit that brings the largest weight to 2^15 (|exp(z - L) - [j = t]| <= 1), so that probabilities down
+// to 2^-29 keep all their bits; unit[0] multiplies, unit[1] takes it back.  bf16 has the range of fp32.
+struct UnitArgs {
+    const float* weight;
+    const int64_t* targets;
+    int n;
+    float* unit;               // null: none is needed
 };
 
 template <bool F32>
-__global__ __launch_bounds__(256) void pack_kernel(PackArgs a) {
+__device__ __forceinline__ void pack(const PackArgs& a, int64_t block) {
     const int64_t chunks = a.ld_out / 8, total = a.rows_out * chunks;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    for (int64_t i = block * 256 + threadIdx.x; i < total; i += (int64_t)a.blocks * 256) {
         const int64_t row = i / chunks;
         const int k0 = (int)(i - row * chunks) * 8;
         bool in = row < a.rows;
@@ -56,8 +65,6 @@ __global__ __launch_bounds__(256) void pack_kernel(PackArgs a) {
                     const uint16_t b = to_bf16(f[e]);
                     o[e] = (short)b;
                     f[e] = f[e] - from_bf16(b);
-                    // (an infinity or NaN is whole in the first plane: inf - inf would make the product of an infinite value NaN)
-                    if ((b & 0x7f80) == 0x7f80) f[e] = 0.f;
                 }
                 *reinterpret_cast<short8v*>(a.dst + p * a.rows_out * a.ld_out + row * a.ld_out + k0) = o;
             }
@@ -76,52 +83,74 @@ __global__ __launch_bounds__(256) void pack_kernel(PackArgs a) {
     }
 }
 
-static int launch_pack(const PackArgs& a, bool f32, hipStream_t st) {
-    const int64_t total = a.rows_out * (a.ld_out / 8);
-    const unsigned grid = (unsigned)std::min<int64_t>((total + 255) / 256, 8192);
-    if (f32) hipLaunchKernelGGL(pack_kernel<true>, dim3(grid), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(pack_kernel<false>, dim3(grid), dim3(256), 0, st, a);
-    IVFR_HIP(hipGetLastError());
-    return IVFR_OK;
+__device__ __forceinline__ void find_unit(const UnitArgs& a) {
+    __shared__ float red[4];
+    float m = 0.f;
+    for (int i = threadIdx.x; i < a.n; i += 256)
+        if (a.targets[i] >= 0) m = fmaxf(m, fabsf(a.weight[i]));
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+        int ex = 0;
+        if (m > 0.f && m < INFINITY) (void)frexpf(m, &ex);   // m < 2^ex
+        ex = min(max(15 - ex, -110), 110);
+        a.unit[0] = ldexpf(1.f, ex);
+        a.unit[1] = ldexpf(1.f, -ex);
+    }
+}
+
+// Both operands and the unit in one launch: the first blocks take x, the next w, the last one the unit.
+template <bool F32>
+__global__ __launch_bounds__(256) void prepare_kernel(PackArgs x, PackArgs w, UnitArgs u) {
+    if (blockIdx.x < x.blocks) pack<F32>(x, blockIdx.x);
+    else if (blockIdx.x < x.blocks + w.blocks) pack<F32>(w, blockIdx.x - x.blocks);
+    else find_unit(u);
 }
 
 // ---------------------------------------------------------------- loss
 
 struct ScoreArgs {
     ProductOperand w, x;       // P, Q
-    ProductPlanes planes;
-    int stages, tiles_p, tiles_q;
+    int planes, slices, tiles_p, tiles_q;
     int v, n;                  // vectors of this piece, rows
     int v0, v_all;             // first vector of this piece; all vectors
-    float scale;
+    float scale;               // times log2 e
     const float* offset;       // of this piece, or null
     const int64_t* targets;
     // loss
-    float2* part;              // [n][tiles_p] (maximum, sum of exponentials relative to it)
+    float2* part;              // [n][tiles_p] (maximum, sum of powers relative to it)
     float* target_score;       // [n]
     // gradient
     const float* lse;          // [n]
     const float* weight;       // [n]
-    const float* unit;         // factor of e, or null
+    const float* unit;         // unit[0] is a factor of e, or null
     uint16_t* e;               // [planes][n_pad][e_ld]
     int64_t e_ld;
     int n_pad, v_pad;          // rows and columns of e that are written (zeros beyond n and v)
 };
 
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+#define LOG2E 1.44269504088896340736f
+#define LN2 0.69314718055994530942f
 
-// scores of this lane's outputs, in place; vectors that take no part, or do not exist: -inf
+// scores of this lane's outputs times log2 e (exponentials are powers of two from here on), in place; vectors that take no part, or do not exist: -inf
 template <class C>
 __device__ __forceinline__ void scores(const ScoreArgs& a, int p0, floatx4 (&acc)[C::TM][C::TN]) {
-    const bool whole = p0 + C::BM <= a.v;
+    if (!a.offset && p0 + C::BM <= a.v) {   // uniform
+#pragma unroll
+        for (int t = 0; t < C::TM; ++t)
+#pragma unroll
+            for (int u = 0; u < C::TN; ++u) acc[t][u] *= a.scale;
+        return;
+    }
 #pragma unroll
     for (int t = 0; t < C::TM; ++t) {
         const int j = p0 + C::p_of(t);
-        float o[4] = {0.f, 0.f, 0.f, 0.f};
-        if (a.offset || !whole) {
+        float o[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[r] = j + r < a.v ? (a.offset ? a.offset[j + r] : 0.f) : -INFINITY;
-        }
+        for (int r = 0; r < 4; ++r) o[r] = j + r < a.v ? (a.offset ? a.offset[j + r] * LOG2E : 0.f) : -INFINITY;
 #pragma unroll
         for (int u = 0; u < C::TN; ++u)
 #pragma unroll
@@ -129,14 +158,26 @@ __device__ __forceinline__ void scores(const ScoreArgs& a, int p0, floatx4 (&acc
     }
 }
 
+// value = f(value) for the output at row `at` of the tile (negative: none) in column u, by the lane that has it.
+template <class C, class F>
+__device__ __forceinline__ void at_row(floatx4 (&acc)[C::TM][C::TN], int u, int at, F f) {
+    const int lane = threadIdx.x & 63, rel = at - (int)(threadIdx.x >> 6) / C::WAVES_N * (C::BM / C::WAVES_M);
+    if (at < 0 || rel < 0 || rel >= C::BM / C::WAVES_M || ((rel >> 3) & 3) != lane >> 4) return;
+#pragma unroll
+    for (int t = 0; t < C::TM; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if ((rel >> 5) * 2 + ((rel >> 2) & 1) == t && (rel & 3) == r) acc[t][u][r] = f(acc[t][u][r]);
+}
+
 template <class C>
-__global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void score_kernel(ScoreArgs a) {
+__global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void score_kernel(ScoreArgs a) {
     __shared__ __align__(1024) char smem[C::LDS];
-    const ProductTile tile = product_tile(a.tiles_p, a.tiles_q, 1);
+    const ProductTile tile = product_tile(blockIdx.x, a.tiles_p, a.tiles_q, 1);
     if (!tile.any) return;   // uniform
     const int p0 = tile.p * C::BM, q0 = tile.q * C::BN;
     floatx4 acc[C::TM][C::TN];
-    C::run(a.w, a.x, a.planes, p0, q0, 0, a.stages, smem, acc);
+    C::run(a.w, a.x, p0, q0, 0, a.slices, smem, acc);
     scores<C>(a, p0, acc);
     __syncthreads();   // the stages are no longer read
     float2* const red = reinterpret_cast<float2*>(smem);   // [WAVES_M][BN]
@@ -145,14 +186,12 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void score_k
     for (int u = 0; u < C::TN; ++u) {
         const int i = q0 + C::q_of(u);
         const int64_t target = i < a.n ? a.targets[i] : -1;
+        at_row<C>(acc, u, target >= p0 && target < a.v && target < p0 + C::BM ? (int)target - p0 : -1, [&](float z) { return a.target_score[i] = z; });   // (one lane of the launch)
         float m = -INFINITY;
 #pragma unroll
         for (int t = 0; t < C::TM; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                m = fmaxf(m, acc[t][u][r]);
-                if (target == (int64_t)p0 + C::p_of(t) + r) a.target_score[i] = acc[t][u][r];   // (one lane of the launch; it has i < n)
-            }
+            for (int r = 0; r < 4; ++r) m = fmaxf(m, acc[t][u][r]);
         m = fmaxf(m, __shfl_xor(m, 16, 64));
         m = fmaxf(m, __shfl_xor(m, 32, 64));
         const float base = m == -INFINITY ? 0.f : m;   // nothing takes part: a sum of zeros, not of NaN
@@ -160,7 +199,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void score_k
 #pragma unroll
         for (int t = 0; t < C::TM; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) s += exp_of(acc[t][u][r] - base);
+            for (int r = 0; r < 4; ++r) s += __builtin_amdgcn_exp2f(acc[t][u][r] - base);
         s += __shfl_xor(s, 16, 64);
         s += __shfl_xor(s, 32, 64);
         if (lane < 16) red[wm * C::BN + C::q_of(u)] = make_float2(m, s);
@@ -175,7 +214,7 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void score_k
         const float base = m == -INFINITY ? 0.f : m;
         float s = 0.f;
 #pragma unroll
-        for (int w = 0; w < C::WAVES_M; ++w) s += red[w * C::BN + q].y * exp_of(red[w * C::BN + q].x - base);
+        for (int w = 0; w < C::WAVES_M; ++w) s += red[w * C::BN + q].y * __builtin_amdgcn_exp2f(red[w * C::BN + q].x - base);
         a.part[(int64_t)i * a.tiles_p + tile.p] = make_float2(m, s);
     }
 }
@@ -190,18 +229,18 @@ __global__ __launch_bounds__(256) void loss_kernel(const float2* __restrict__ pa
     for (int t = lane; t < tiles; t += 64) {
         const float2 x = p[t];
         const float top = fmaxf(m, x.x), base = top == -INFINITY ? 0.f : top;
-        s = s * exp_of(m - base) + x.y * exp_of(x.x - base);
+        s = s * __builtin_amdgcn_exp2f(m - base) + x.y * __builtin_amdgcn_exp2f(x.x - base);
         m = top;
     }
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) {
         const float om = __shfl_xor(m, off, 64), os = __shfl_xor(s, off, 64);
         const float top = fmaxf(m, om), base = top == -INFINITY ? 0.f : top;
-        s = s * exp_of(m - base) + os * exp_of(om - base);
+        s = s * __builtin_amdgcn_exp2f(m - base) + os * __builtin_amdgcn_exp2f(om - base);
         m = top;
     }
     if (lane == 0) {
-        const float ls = logf(s), L = m == -INFINITY && s == 0.f ? -INFINITY : m + ls;
+        const float ls = log2f(s), L = m == -INFINITY && s == 0.f ? -INFINITY : (m + ls) * LN2;
         if (lse) lse[i] = L;
         if (loss) {
             const int64_t t = targets[i];
@@ -210,7 +249,7 @@ __global__ __launch_bounds__(256) void loss_kernel(const float2* __restrict__ pa
             else if (t >= v) x = NAN;
             else {
                 const float z = target_score[i];
-                x = z == -INFINITY ? INFINITY : (m - z) + ls;
+                x = z == -INFINITY ? INFINITY : ((m - z) + ls) * LN2;
             }
             loss[i] = x;
         }
@@ -219,35 +258,14 @@ __global__ __launch_bounds__(256) void loss_kernel(const float2* __restrict__ pa
 
 // ---------------------------------------------------------------- gradient
 
-// fp16 calls: e is written in a unit that brings the largest weight to 2^15 (|exp(z - L) - [j = t]| <= 1), so that probabilities down
-// to 2^-29 keep all their bits; unit[0] multiplies, unit[1] takes it back.  bf16 has the range of fp32.
-__global__ __launch_bounds__(256) void weight_unit_kernel(const float* __restrict__ weight, const int64_t* __restrict__ targets, int n, float* __restrict__ unit) {
-    __shared__ float red[4];
-    float m = 0.f;
-    for (int i = threadIdx.x; i < n; i += 256)
-        if (targets[i] >= 0) m = fmaxf(m, fabsf(weight[i]));
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-        int ex = 0;
-        if (m > 0.f && m < INFINITY) (void)frexpf(m, &ex);   // m < 2^ex
-        ex = min(max(15 - ex, -110), 110);
-        unit[0] = ldexpf(1.f, ex);
-        unit[1] = ldexpf(1.f, -ex);
-    }
-}
-
-template <class C, int PLANES>
-__global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void grad_score_kernel(ScoreArgs a) {
+template <class C>
+__global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void grad_score_kernel(ScoreArgs a) {
     __shared__ __align__(1024) char smem[C::LDS];
-    const ProductTile tile = product_tile(a.tiles_p, a.tiles_q, 1);
+    const ProductTile tile = product_tile(blockIdx.x, a.tiles_p, a.tiles_q, 1);
     if (!tile.any) return;   // uniform
     const int p0 = tile.p * C::BM, q0 = tile.q * C::BN;
     floatx4 acc[C::TM][C::TN];
-    C::run(a.w, a.x, a.planes, p0, q0, 0, a.stages, smem, acc);
+    C::run(a.w, a.x, p0, q0, 0, a.slices, smem, acc);
     scores<C>(a, p0, acc);
     const float unit = a.unit ? a.unit[0] : 1.f;
 #pragma unroll
@@ -259,23 +277,30 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void grad_sc
         if (i < a.n) {
             target = a.targets[i];
             L = a.lse[i];
-            g = target < 0 ? 0.f : (a.weight[i] != 0.f && target >= a.v_all ? NAN : a.weight[i] * unit);
+            if (L == -INFINITY) L = 0.f;   // nothing takes part: powers of -inf, not NaN
+            g = target < 0 ? 0.f : a.weight[i] * unit;
+            if (target >= a.v_all && g != 0.f) g = NAN;
         }
-        const int at = target >= a.v0 && target - a.v0 < a.v ? (int)(target - a.v0) : -1;
+#pragma unroll
+        for (int t = 0; t < C::TM; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[t][u][r] = __builtin_amdgcn_exp2f(fmaf(L, -LOG2E, acc[t][u][r]));
+        {   // the row's own vector, if it is in this tile and takes part: p - 1 before anything is rounded
+            int at = target >= (int64_t)a.v0 + p0 && target < (int64_t)a.v0 + a.v && target < (int64_t)a.v0 + p0 + C::BM ? (int)(target - a.v0 - p0) : -1;
+            if (at >= 0 && a.offset && a.offset[p0 + at] == -INFINITY) at = -1;
+            at_row<C>(acc, u, at, [](float p) { return p - 1.f; });
+        }
+        const bool live = g != 0.f;   // (a row without gradient: zeros, whatever its statistics are)
 #pragma unroll
         for (int t = 0; t < C::TM; t += 2) {
             const int j = p0 + C::p_of(t);
             if (j >= a.v_pad) continue;   // (a multiple of 8, as j)
             float f[8];
 #pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                const float z = acc[t + (r >> 2)][u][r & 3];
-                const float x = g * (exp_of(z - L) - (j + r == at ? 1.f : 0.f));
-                f[r] = z == -INFINITY || g == 0.f ? 0.f : x;
-            }
+            for (int r = 0; r < 8; ++r) f[r] = g * acc[t + (r >> 2)][u][r & 3];
             uint16_t* const o = a.e + (int64_t)i * a.e_ld + j;
 #pragma unroll
-            for (int p = 0; p < PLANES; ++p) {
+            for (int p = 0; p < C::PLANES; ++p) {
                 short8v h;
 #pragma unroll
                 for (int r = 0; r < 8; ++r) {
@@ -283,9 +308,10 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void grad_sc
                     else {
                         const uint16_t b = to_bf16(f[r]);
                         h[r] = (short)b;
-                        f[r] -= from_bf16(b);
+                        if constexpr (C::PLANES > 1) f[r] -= from_bf16(b);
                     }
                 }
+                if (!live) h = short8v{0, 0, 0, 0, 0, 0, 0, 0};
                 *reinterpret_cast<short8v*>(o + (int64_t)p * a.n_pad * a.e_ld) = h;
             }
         }
@@ -294,75 +320,54 @@ __global__ __launch_bounds__(C::THREADS, C::THREADS == 512 ? 2 : 1) void grad_sc
 
 // ---------------------------------------------------------------- host
 
-// The tile by the sizes: few rows read the vectors once and are bound by that; else 256 x 256 where these give every compute unit a tile.
-struct ScoreKind {
-    int bm, bn;
-};
-static const ScoreKind SCORE_KINDS[] = {{256, 256}, {128, 128}, {256, 64}, {256, 16}};
-
-static int score_kind(int64_t n, int64_t v, int n_cu) {
-    if (n <= 16) return 3;
-    if (n <= 64) return 2;
-    return ((n + 255) / 256) * ((v + 255) / 256) >= n_cu ? 0 : 1;
+// The tile by the sizes: few rows read the vectors once and are bound by that; else the largest tile that gives the compute units work.
+static int score_tile(int64_t n, int64_t v, int planes) {
+    if (n <= 16) return IVFR_TILE_256x16;
+    if (n <= 64) return IVFR_TILE_256x64;
+    if (planes == 1 && ((n + 127) / 128) * ((v + 255) / 256) >= IVFR_PRODUCT_CU) return IVFR_TILE_256x128;
+    return ((n + 127) / 128) * ((v + 127) / 128) >= IVFR_PRODUCT_CU / 2 ? IVFR_TILE_128x128 : IVFR_TILE_64x64;
 }
 
-template <class C>
-static int launch_score(const ScoreArgs& a, hipStream_t st) {
-    hipLaunchKernelGGL((score_kernel<C>), dim3(product_grid((int64_t)a.tiles_p * a.tiles_q)), dim3(C::THREADS), 0, st, a);
+template <int TILE, bool HALF, int PLANES>
+static int launch_score_tile(const ScoreArgs& a, bool grad, hipStream_t st) {
+    typedef typename ProductOf<TILE, false, false, HALF, PLANES>::T C;
+    const dim3 grid(product_grid((int64_t)a.tiles_p * a.tiles_q));
+    if (grad) hipLaunchKernelGGL((grad_score_kernel<C>), grid, dim3(C::THREADS), 0, st, a);
+    else hipLaunchKernelGGL((score_kernel<C>), grid, dim3(C::THREADS), 0, st, a);
     IVFR_HIP(hipGetLastError());
     return IVFR_OK;
 }
-template <class C>
-static int launch_grad_score(const ScoreArgs& a, hipStream_t st) {
-    if constexpr (!C::HALF)
-        if (a.planes.n > 1) {
-            hipLaunchKernelGGL((grad_score_kernel<C, 3>), dim3(product_grid((int64_t)a.tiles_p * a.tiles_q)), dim3(C::THREADS), 0, st, a);
-            IVFR_HIP(hipGetLastError());
-            return IVFR_OK;
-        }
-    hipLaunchKernelGGL((grad_score_kernel<C, 1>), dim3(product_grid((int64_t)a.tiles_p * a.tiles_q)), dim3(C::THREADS), 0, st, a);
-    IVFR_HIP(hipGetLastError());
-    return IVFR_OK;
-}
-template <bool HALF, bool GRAD>
-static int launch_scores_of(ScoreArgs& a, int kind, hipStream_t st) {
-    a.tiles_p = (int)(((GRAD ? a.v_pad : a.v) + SCORE_KINDS[kind].bm - 1) / SCORE_KINDS[kind].bm);
-    a.tiles_q = (int)(((GRAD ? a.n_pad : a.n) + SCORE_KINDS[kind].bn - 1) / SCORE_KINDS[kind].bn);
-    typedef Product<256, 256, 2, 4, false, false, HALF> K0;
-    typedef Product<128, 128, 2, 2, false, false, HALF> K1;
-    typedef Product<256, 64, 8, 1, false, false, HALF> K2;
-    typedef Product<256, 16, 8, 1, false, false, HALF> K3;
-    if constexpr (GRAD) {
-        switch (kind) {
-            case 0: return launch_grad_score<K0>(a, st);
-            case 1: return launch_grad_score<K1>(a, st);
-            case 2: return launch_grad_score<K2>(a, st);
-            default: return launch_grad_score<K3>(a, st);
-        }
-    } else {
-        switch (kind) {
-            case 0: return launch_score<K0>(a, st);
-            case 1: return launch_score<K1>(a, st);
-            case 2: return launch_score<K2>(a, st);
-            default: return launch_score<K3>(a, st);
-        }
+template <bool HALF, int PLANES>
+static int launch_score_planes(const ScoreArgs& a, int tile, bool grad, hipStream_t st) {
+    switch (tile) {
+        case IVFR_TILE_256x128:
+            if constexpr (PLANES == 1) return launch_score_tile<IVFR_TILE_256x128, HALF, 1>(a, grad, st);
+            break;
+        case IVFR_TILE_128x128: return launch_score_tile<IVFR_TILE_128x128, HALF, PLANES>(a, grad, st);
+        case IVFR_TILE_64x64: return launch_score_tile<IVFR_TILE_64x64, HALF, PLANES>(a, grad, st);
+        case IVFR_TILE_256x64: return launch_score_tile<IVFR_TILE_256x64, HALF, PLANES>(a, grad, st);
+        case IVFR_TILE_256x16: return launch_score_tile<IVFR_TILE_256x16, HALF, PLANES>(a, grad, st);
     }
+    ivfr_set_error("softmax: no such tile: %d", tile);
+    return IVFR_ERR_INVALID_ARG;
 }
-static int launch_scores(ScoreArgs& a, int kind, bool half, bool grad, hipStream_t st) {
-    if (half) return grad ? launch_scores_of<true, true>(a, kind, st) : launch_scores_of<true, false>(a, kind, st);
-    return grad ? launch_scores_of<false, true>(a, kind, st) : launch_scores_of<false, false>(a, kind, st);
+static int launch_scores(ScoreArgs& a, int tile, bool half, bool grad, hipStream_t st) {
+    a.tiles_p = ((grad ? a.v_pad : a.v) + IVFR_TILE_P[tile] - 1) / IVFR_TILE_P[tile];
+    a.tiles_q = ((grad ? a.n_pad : a.n) + IVFR_TILE_Q[tile] - 1) / IVFR_TILE_Q[tile];
+    if (a.planes == 3) return launch_score_planes<false, 3>(a, tile, grad, st);
+    return half ? launch_score_planes<true, 1>(a, tile, grad, st) : launch_score_planes<false, 1>(a, tile, grad, st);
 }
 
 static inline int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 // What a call keeps in its workspace, and where.
 struct SoftmaxPlan {
-    int planes, stages, kind, n_cu;
+    int planes, slices, tile;
     bool half, pack_x, pack_w;
     int64_t kd, n_pad, e_ld, piece;   // columns of packed operands; rows and columns of e, vectors a piece
     int pieces;
     int64_t tiles_p;                  // of the loss
-    ProductPlan dx, dw;               // of a whole piece
+    int dx_tile, dx_splits, dw_tile, dw_splits;   // of a whole piece
     int64_t at_x, at_w, at_part, at_target, at_lse, at_unit, at_e, at_dx, at_dw, bytes;
 };
 
@@ -382,14 +387,12 @@ static int softmax_check(const ivfr_softmax_args* a) {
 
 static SoftmaxPlan softmax_plan(const ivfr_softmax_args& a, bool grad) {
     SoftmaxPlan p = {};
-    p.n_cu = IVFR_PRODUCT_CU;
     const bool f32 = a.type == IVFR_TYPE_F32;
     p.half = a.type == IVFR_TYPE_F16;
     p.planes = f32 ? 3 : 1;
     p.kd = round_up(a.d, 32);
-    p.stages = (int)(p.kd / 32);
+    p.slices = (int)(p.kd / 32);
     p.n_pad = round_up(a.n, 32);
-    const int pairs = product_planes(p.planes).n;
     // gradients read x by rows of k: padded to whole stages; rows that take no part are zeroed in the copy
     p.pack_x = f32 || grad || a.d % 32 || !rows_aligned(a.x, a.ldx, 2);
     p.pack_w = f32 || (grad && a.offset) || a.d % 32 || !rows_aligned(a.w, a.ldw, 2);
@@ -401,8 +404,8 @@ static SoftmaxPlan softmax_plan(const ivfr_softmax_args& a, bool grad) {
     };
     if (p.pack_x) p.at_x = take(p.planes * (grad ? p.n_pad : a.n) * p.kd * 2);
     if (p.pack_w) p.at_w = take(p.planes * a.v * p.kd * 2);
-    p.kind = score_kind(a.n, a.v, p.n_cu);
-    p.tiles_p = (a.v + SCORE_KINDS[p.kind].bm - 1) / SCORE_KINDS[p.kind].bm;
+    p.tile = score_tile(a.n, a.v, p.planes);
+    p.tiles_p = (a.v + IVFR_TILE_P[p.tile] - 1) / IVFR_TILE_P[p.tile];
     p.at_part = take(a.n * p.tiles_p * 8);
     p.at_target = take(a.n * 4);
     if (grad) {
@@ -413,12 +416,12 @@ static SoftmaxPlan softmax_plan(const ivfr_softmax_args& a, bool grad) {
         p.pieces = (int)((a.v + fit - 1) / fit);
         p.piece = std::min(round_up((a.v + p.pieces - 1) / p.pieces, 256), round_up(a.v, 32));
         p.pieces = (int)((a.v + p.piece - 1) / p.piece);
-        p.e_ld = round_up(p.piece, 64);
+        p.e_ld = round_up(p.piece, 64) + 64;   // (not a large power of two: rows would all begin in the same memory channel)
         p.at_e = take(p.planes * p.n_pad * p.e_ld * 2);
-        p.dx = product_plan(a.d, a.n, (p.piece + 31) / 32, pairs, false, p.n_cu);
-        p.dw = product_plan(a.d, p.piece, p.n_pad / 32, pairs, true, p.n_cu);
-        if (p.pieces > 1 || p.dx.splits > 1) p.at_dx = take((int64_t)p.pieces * p.dx.splits * a.n * product_pad(a.d) * 4);
-        if (p.dw.splits > 1) p.at_dw = take(p.dw.splits * p.piece * product_pad(a.d) * 4);
+        product_cut(a.d, a.n, (p.piece + 31) / 32, p.planes, false, &p.dx_tile, &p.dx_splits);
+        product_cut(a.d, p.piece, p.n_pad / 32, p.planes, true, &p.dw_tile, &p.dw_splits);
+        if (p.pieces > 1 || p.dx_splits > 1) p.at_dx = take((int64_t)p.pieces * p.dx_splits * a.n * product_pad(a.d) * 4);
+        if (p.dw_splits > 1) p.at_dw = take(p.dw_splits * p.piece * product_pad(a.d) * 4);
     }
     p.bytes = at;
     return p;
@@ -442,40 +445,48 @@ static int softmax_pointers(const ivfr_softmax_args& a, const SoftmaxPlan& p, co
     return IVFR_OK;
 }
 
-static int pack_operands(const ivfr_softmax_args& a, const SoftmaxPlan& p, bool grad, char* ws, ScoreArgs& s, hipStream_t st) {
+// weight: of a gradient, else null
+static int prepare(const ivfr_softmax_args& a, const SoftmaxPlan& p, const float* weight, char* ws, ScoreArgs& s, hipStream_t st) {
     const bool f32 = a.type == IVFR_TYPE_F32;
     s.x = {(const uint16_t*)a.x, 0, a.ldx, (int)a.n, 0};
     s.w = {(const uint16_t*)a.w, 0, a.ldw, (int)a.v, 0};
+    PackArgs x = {}, w = {};
+    UnitArgs u = {};
+    auto blocks = [](const PackArgs& k) { return (unsigned)std::min<int64_t>((k.rows_out * (k.ld_out / 8) + 255) / 256, 4096); };
     if (p.pack_x) {
-        PackArgs k = {a.x, a.ldx, a.n, grad ? p.n_pad : a.n, p.kd, a.d, p.planes, rows_aligned(a.x, a.ldx, f32 ? 4 : 2), (uint16_t*)(ws + p.at_x),
-                      nullptr, grad ? a.targets : nullptr};
-        IVFR_TRY(launch_pack(k, f32, st));
-        s.x.base = k.dst;
-        s.x.ld = p.kd;
-        s.x.plane = k.rows_out * p.kd;
-        s.x.extent = (int)k.rows_out;   // (the rows of e reach up to the padding)
+        x = {a.x, a.ldx, a.n, weight ? p.n_pad : a.n, p.kd, a.d, rows_aligned(a.x, a.ldx, f32 ? 4 : 2), (uint16_t*)(ws + p.at_x), nullptr, weight ? a.targets : nullptr, 0};
+        x.blocks = blocks(x);
+        s.x = {x.dst, x.rows_out * p.kd, p.kd, (int)x.rows_out, 0};   // (the rows of e reach up to the padding)
     }
     if (p.pack_w) {
-        PackArgs k = {a.w, a.ldw, a.v, a.v, p.kd, a.d, p.planes, rows_aligned(a.w, a.ldw, f32 ? 4 : 2), (uint16_t*)(ws + p.at_w), a.offset, nullptr};
-        IVFR_TRY(launch_pack(k, f32, st));
-        s.w.base = k.dst;
-        s.w.ld = p.kd;
-        s.w.plane = a.v * p.kd;
+        w = {a.w, a.ldw, a.v, a.v, p.kd, a.d, rows_aligned(a.w, a.ldw, f32 ? 4 : 2), (uint16_t*)(ws + p.at_w), a.offset, nullptr, 0};
+        w.blocks = blocks(w);
+        s.w = {w.dst, a.v * p.kd, p.kd, (int)a.v, 0};
     }
-    s.planes = product_planes(p.planes);
-    s.stages = p.stages;
+    if (weight && p.half) {
+        u = {weight, a.targets, (int)a.n, (float*)(ws + p.at_unit)};
+        s.unit = u.unit;
+    }
+    if (const unsigned grid = x.blocks + w.blocks + (u.unit ? 1 : 0)) {
+        if (f32) hipLaunchKernelGGL(prepare_kernel<true>, dim3(grid), dim3(256), 0, st, x, w, u);
+        else hipLaunchKernelGGL(prepare_kernel<false>, dim3(grid), dim3(256), 0, st, x, w, u);
+        IVFR_HIP(hipGetLastError());
+    }
+    s.planes = p.planes;
+    s.slices = p.slices;
     s.n = (int)a.n;
     s.v = s.v_all = (int)a.v;
-    s.scale = a.scale;
+    s.scale = a.scale * LOG2E;
     s.offset = a.offset;
     s.targets = a.targets;
+    s.weight = weight;
     s.part = (float2*)(ws + p.at_part);
     s.target_score = (float*)(ws + p.at_target);
     return IVFR_OK;
 }
 
 static int statistics(const ivfr_softmax_args& a, const SoftmaxPlan& p, ScoreArgs s, float* loss, float* lse, hipStream_t st) {
-    IVFR_TRY(launch_scores(s, p.kind, p.half, false, st));
+    IVFR_TRY(launch_scores(s, p.tile, p.half, false, st));
     hipLaunchKernelGGL(loss_kernel, dim3((unsigned)((a.n + 3) / 4)), dim3(256), 0, st, s.part, (int)p.tiles_p, s.target_score, a.targets, (int)a.n, a.v, loss, lse);
     IVFR_HIP(hipGetLastError());
     return IVFR_OK;
@@ -490,7 +501,7 @@ int ivfr_softmax_loss(const ivfr_softmax_args* args, float* loss, float* lse, vo
     IVFR_HIP(hipSetDevice(args->device));
     hipStream_t st = (hipStream_t)stream;
     ScoreArgs s = {};
-    IVFR_TRY(pack_operands(*args, p, false, (char*)workspace, s, st));
+    IVFR_TRY(prepare(*args, p, nullptr, (char*)workspace, s, st));
     return statistics(*args, p, s, loss, lse, st);
 }
 
@@ -503,7 +514,7 @@ int ivfr_softmax_loss_grad(const ivfr_softmax_args* args, const float* weight, c
                            void* workspace, int64_t workspace_bytes, void* stream) {
     IVFR_TRY(softmax_check(args));
     const ivfr_softmax_args& a = *args;
-    const int size = a.type == IVFR_TYPE_F32 ? 4 : 2, out_type = a.type;
+    const int size = a.type == IVFR_TYPE_F32 ? 4 : 2;
     hipStream_t st = (hipStream_t)stream;
     IVFR_REQUIRE(dw && ((uintptr_t)dw & 15) == 0, "softmax: dw must be aligned to 16 bytes");
     if (a.n == 0) {   // no rows: no gradient
@@ -520,25 +531,19 @@ int ivfr_softmax_loss_grad(const ivfr_softmax_args* args, const float* weight, c
     IVFR_HIP(hipSetDevice(a.device));
     char* const ws = (char*)workspace;
     ScoreArgs s = {};
-    IVFR_TRY(pack_operands(a, p, true, ws, s, st));
-    float* const unit = p.half ? (float*)(ws + p.at_unit) : nullptr;
-    if (unit) {
-        hipLaunchKernelGGL(weight_unit_kernel, dim3(1), dim3(256), 0, st, weight, a.targets, (int)a.n, unit);
-        IVFR_HIP(hipGetLastError());
-    }
+    IVFR_TRY(prepare(a, p, weight, ws, s, st));
     if (!lse || loss) {
         float* const own_lse = (float*)(ws + p.at_lse);
         IVFR_TRY(statistics(a, p, s, loss, own_lse, st));
         if (!lse) lse = own_lse;
     }
     s.lse = lse;
-    s.weight = weight;
-    s.unit = unit;
     s.e = (uint16_t*)(ws + p.at_e);
     s.e_ld = p.e_ld;
     s.n_pad = (int)p.n_pad;
-    const bool parts = p.pieces > 1 || p.dx.splits > 1;
-    const ProductOperand x = s.x, w = s.w;
+    const bool parts = p.pieces > 1 || p.dx_splits > 1;
+    const ProductOperand w = s.w;
+    ProductOut ox = {}, ow = {};
     for (int i = 0; i < p.pieces; ++i) {
         const int64_t v0 = (int64_t)i * p.piece, here = std::min(p.piece, a.v - v0);
         s.v0 = (int)v0;
@@ -548,41 +553,40 @@ int ivfr_softmax_loss_grad(const ivfr_softmax_args* args, const float* weight, c
         s.w.base = w.base + v0 * w.ld;
         s.w.extent = (int)here;
         s.offset = a.offset ? a.offset + v0 : nullptr;
-        IVFR_TRY(launch_scores(s, score_kind(a.n, here, p.n_cu), p.half, true, st));
-        ProductOut o = {};
-        o.half = p.half;
-        o.planes = s.planes;
-        o.type = out_type;
-        o.alpha = a.scale;
-        o.unit = unit;
-        o.np = a.d;
-        o.ld = a.d;
+        IVFR_TRY(launch_scores(s, score_tile(a.n, here, p.planes), p.half, true, st));
+        ox.planes = s.planes;
+        ox.type = a.type;
+        ox.alpha = a.scale;
+        ox.unit = s.unit;
+        ox.np = a.d;
+        ox.ld = a.d;
+        ow = ox;
         // dx [n, d]: over the vectors of the piece
-        o.P = s.w;
-        o.P.extent = a.d;
-        o.P.rows = (int)here;
-        o.Q = {s.e, p.n_pad * p.e_ld, p.e_ld, (int)a.n, 0};
-        o.q_outer = false;
-        o.stages = s.v_pad / 32;
-        o.nq = (int)a.n;
-        o.out = dx;
-        o.partial = parts ? (float*)(ws + p.at_dx) : nullptr;
-        o.slot0 = i * p.dx.splits;
-        IVFR_TRY(product_launch(o, p.dx, st));
+        ox.P = s.w;
+        ox.P.extent = a.d;
+        ox.P.rows = (int)here;
+        ox.Q = {s.e, p.n_pad * p.e_ld, p.e_ld, (int)a.n, 0};
+        ox.slices = s.v_pad / 32;
+        ox.nq = (int)a.n;
+        ox.out = dx;
+        ox.partial = parts ? (float*)(ws + p.at_dx) : nullptr;
+        ox.slot0 = i * p.dx_splits;
+        ox.tile = p.dx_tile;
+        ox.splits = p.dx_splits;
         // dw [here, d]: over the rows
-        o.P = x;
-        o.P.extent = a.d;
-        o.P.rows = (int)p.n_pad;
-        o.Q = {s.e, p.n_pad * p.e_ld, p.e_ld, (int)here, (int)p.n_pad};
-        o.q_outer = true;
-        o.stages = (int)(p.n_pad / 32);
-        o.nq = (int)here;
-        o.out = (char*)dw + v0 * a.d * size;
-        o.partial = p.dw.splits > 1 ? (float*)(ws + p.at_dw) : nullptr;
-        o.slot0 = 0;
-        IVFR_TRY(product_launch(o, p.dw, st));
-        if (p.dw.splits > 1) IVFR_TRY(product_join(o.partial, p.dw.splits, here, a.d, out_type, a.scale, unit, o.out, a.d, st));
+        ow.P = s.x;
+        ow.P.extent = a.d;
+        ow.P.rows = (int)p.n_pad;
+        ow.Q = {s.e, p.n_pad * p.e_ld, p.e_ld, (int)here, (int)p.n_pad};
+        ow.slices = (int)(p.n_pad / 32);
+        ow.nq = (int)here;
+        ow.out = (char*)dw + v0 * a.d * size;
+        ow.partial = p.dw_splits > 1 ? (float*)(ws + p.at_dw) : nullptr;
+        ow.slot0 = 0;
+        ow.tile = p.dw_tile;
+        ow.splits = p.dw_splits;
+        IVFR_TRY(product_launch(ox, ow, p.half, st));
+        IVFR_TRY(product_join(ox, parts && i + 1 == p.pieces ? p.pieces * p.dx_splits : 0, ow, p.dw_splits > 1 ? p.dw_splits : 0, st));
     }
-    if (parts) IVFR_TRY(product_join((float*)(ws + p.at_dx), p.pieces * p.dx.splits, a.n, a.d, out_type, a.scale, unit, dx, a.d, st));
     return IVFR_OK;
 }
