@@ -16,12 +16,13 @@
 #include <cmath>
 
 #define ORTHO_SCALE 4096.f
-#define ORTHO_SUMS 64          // workgroups that sum the squares of a matrix
+#define ORTHO_SUMS 256         // workgroups at most that sum the squares of a matrix
 
 struct OrthoPlan {
     int r, c, rp, cp, planes;
-    bool tall, half;
+    bool tall, small;
     int64_t batch;
+    int parts;
     int64_t at_sums, at_x[2], at_a, at_b, bytes;
     int64_t xsize, asize;      // elements of a plane of one matrix
 };
@@ -30,10 +31,11 @@ struct MatrixArgs {
     const void* g;
     int64_t ld, batch_stride;
     int rows, cols, type;      // of g
-    int tall, rp, cp, planes;
+    int tall, rp, cp, planes, vec;   // vec: rows start at 16-byte boundaries
     int64_t xsize;             // elements of a plane; a matrix has `planes` of them
     float eps;
-    double* sums;              // [batch][ORTHO_SUMS]
+    double* sums;              // [batch][parts]
+    int parts;
     uint16_t* x;
     void* out;                 // dense, as g
     float out_scale;
@@ -56,35 +58,57 @@ __device__ __forceinline__ void store_planes(uint16_t* p, int64_t plane, int pla
 }
 __device__ __forceinline__ float load_planes(const uint16_t* p, int64_t plane, int planes) { return from_half(p[0]) + (planes > 1 ? from_half(p[plane]) : 0.f); }
 
-// Sums of squares, in fp64 (squares of fp32 values need not fit fp32), in a fixed order.
-__global__ __launch_bounds__(256) void squares_kernel(MatrixArgs a) {
-    __shared__ double red[4];
-    const int64_t total = (int64_t)a.rows * a.cols, base = (int64_t)blockIdx.y * a.batch_stride;
-    double s = 0.0;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += ORTHO_SUMS * 256) {
-        const int64_t row = i / a.cols;
-        const double v = load_value(a.g, base + row * a.ld + (i - row * a.cols), a.type);
-        s += v * v;
-    }
+// sum over 256 threads, in a fixed order, for all of them
+__device__ __forceinline__ double sum_256(double s, double* red) {
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off, 64);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
     __syncthreads();
-    if (threadIdx.x == 0) a.sums[(int64_t)blockIdx.y * ORTHO_SUMS + blockIdx.x] = red[0] + red[1] + red[2] + red[3];
+    return red[0] + red[1] + red[2] + red[3];
+}
+
+// eight values of a row from column k (zeros past the end)
+__device__ __forceinline__ void load_eight(const MatrixArgs& a, int64_t row, int k, float (&f)[8]) {
+    const int64_t at = row * a.ld + k;
+    if (a.vec && k + 8 <= a.cols) {
+        if (a.type == IVFR_TYPE_F32) {
+            const float4 u = *reinterpret_cast<const float4*>((const float*)a.g + at), v = *reinterpret_cast<const float4*>((const float*)a.g + at + 4);
+            f[0] = u.x; f[1] = u.y; f[2] = u.z; f[3] = u.w; f[4] = v.x; f[5] = v.y; f[6] = v.z; f[7] = v.w;
+        } else {
+            const short8v h = *reinterpret_cast<const short8v*>((const uint16_t*)a.g + at);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = a.type == IVFR_TYPE_F16 ? from_half((uint16_t)h[e]) : from_bf16((uint16_t)h[e]);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = k + e < a.cols ? load_value(a.g, at + e, a.type) : 0.f;
+    }
+}
+
+// Sums of squares, in fp64 (squares of fp32 values need not fit fp32), in a fixed order.  Bound by reading g.
+__global__ __launch_bounds__(256) void squares_kernel(MatrixArgs a) {
+    __shared__ double red[4];
+    a.g = (const char*)a.g + (int64_t)blockIdx.y * a.batch_stride * (a.type == IVFR_TYPE_F32 ? 4 : 2);
+    const uint32_t chunks = (uint32_t)(a.cols + 7) / 8;
+    const int64_t total = (int64_t)a.rows * chunks;
+    double s = 0.0;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)a.parts * 256) {
+        const int64_t row = total < (1ll << 32) ? (uint32_t)i / chunks : i / chunks;
+        float f[8];
+        load_eight(a, row, (int)(i - row * chunks) * 8, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s += (double)f[e] * f[e];
+    }
+    s = sum_256(s, red);
+    if (threadIdx.x == 0) a.sums[(int64_t)blockIdx.y * a.parts + blockIdx.x] = s;
 }
 
 // 64 x 64 values of X, through LDS where g is transposed
 __global__ __launch_bounds__(256) void fill_kernel(MatrixArgs a) {
     __shared__ float tile[64][65];
-    __shared__ double inv_s;
-    if (threadIdx.x < 64) {
-        double s = a.sums[(int64_t)blockIdx.z * ORTHO_SUMS + threadIdx.x];
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off, 64);
-        if (threadIdx.x == 0) inv_s = (double)ORTHO_SCALE / (sqrt(s) + (double)a.eps);
-    }
-    __syncthreads();
-    const double inv = inv_s;
+    __shared__ double red[4];
+    const double norm2 = sum_256((int)threadIdx.x < a.parts ? a.sums[(int64_t)blockIdx.z * a.parts + threadIdx.x] : 0.0, red);
+    const double inv = (double)ORTHO_SCALE / (sqrt(norm2) + (double)a.eps);
     const int c0 = blockIdx.x * 64, r0 = blockIdx.y * 64, r = a.tall ? a.cols : a.rows, c = a.tall ? a.rows : a.cols;
     const int64_t base = (int64_t)blockIdx.z * a.batch_stride;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -247,6 +271,211 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void update_kernel(StepA
     }
 }
 
+// ---------------------------------------------------------------- small matrices
+
+// All steps of a matrix in one workgroup, X and A (then B, in its place) in LDS: no launch and no memory in between.  A wavefront has
+// sixteen rows of the outputs and blocks of 32 of their columns (with fewer than 128 rows several wavefronts share the columns of the same rows), so
+// that it reads a fragment of its rows once for all blocks; results stay in registers until all have read what they replace.  Rows
+// in LDS are an odd number of 16-byte chunks long, so that the same chunk of sixteen rows lies in different banks.
+#define SMALL_BLOCKS 8         // that a wavefront holds at most
+#define SMALL_WAVES 16
+
+__host__ __device__ inline int small_pitch(int k) { return 2 * k + 16; }   // bytes
+inline int small_blocks(int rp, int cp) { return (cp / 32 + SMALL_WAVES / (rp / 16) - 1) / (SMALL_WAVES / (rp / 16)); }   // of a wavefront
+inline int64_t small_lds(int rp, int cp, int planes) { return (int64_t)planes * rp * (small_pitch(cp) + small_pitch(rp)); }
+
+struct SmallArgs {
+    MatrixArgs m;
+    float k[64][3];
+    int steps;
+};
+
+struct Inner { static constexpr bool value = false; };   // how an operand lies
+struct Outer { static constexpr bool value = true; };
+
+template <int PLANES, int BLOCKS, int LDS>
+__global__ __launch_bounds__(64 * SMALL_WAVES, SMALL_WAVES / 4) void small_kernel(const SmallArgs a) {
+    __shared__ __align__(16) char smem[LDS];
+    __shared__ double red[SMALL_WAVES];
+    MatrixArgs m = a.m;
+    const int rp = m.rp, cp = m.cp, xpitch = small_pitch(cp), apitch = small_pitch(rp);
+    const int xplane = rp * xpitch, aplane = rp * apitch;
+    char* const X = smem;
+    char* const A = smem + PLANES * xplane;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const int size = m.type == IVFR_TYPE_F32 ? 4 : 2;
+    m.g = (const char*)m.g + (int64_t)blockIdx.x * m.batch_stride * size;
+    m.out = (char*)m.out + (int64_t)blockIdx.x * m.rows * m.cols * size;
+    // the norm, then X; columns of g past the end are read as zeros, rows are padded here
+    const int chunks = (m.cols + 7) / 8, total = m.rows * chunks;
+    double s = 0.0;
+    for (int i = threadIdx.x; i < total; i += 64 * SMALL_WAVES) {
+        float f[8];
+        load_eight(m, i / chunks, i % chunks * 8, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s += (double)f[e] * f[e];
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off, 64);
+    if (lane == 0) red[wave] = s;
+    for (int i = threadIdx.x; i < PLANES * xplane / 16; i += 64 * SMALL_WAVES) reinterpret_cast<uint4*>(X)[i] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+    s = 0.0;
+#pragma unroll
+    for (int w = 0; w < SMALL_WAVES; ++w) s += red[w];
+    const double inv = (double)ORTHO_SCALE / (sqrt(s) + (double)m.eps);
+    for (int i = threadIdx.x; i < total; i += 64 * SMALL_WAVES) {
+        const int row = i / chunks, k = i % chunks * 8;
+        float f[8];
+        load_eight(m, row, k, f);
+#pragma unroll
+        for (int n = 0; n < PLANES; ++n) {
+            short8v h;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float v = n == 0 ? (float)(f[e] * inv) : f[e];
+                const uint16_t b = to_half(v);
+                h[e] = (short)b;
+                f[e] = v - from_half(b);
+            }
+            if (m.tall) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (k + e < m.cols) *reinterpret_cast<uint16_t*>(X + n * xplane + (k + e) * xpitch + 2 * row) = (uint16_t)h[e];
+            } else *reinterpret_cast<short8v*>(X + n * xplane + row * xpitch + 2 * k) = h;   // (the row is padded to 32 columns)
+        }
+    }
+    __syncthreads();
+    typedef Product<64, 64, 2, 2, false, false, true, 1, 1, 3> Unit;   // for its matrix instruction
+    // this wavefront's rows q0 .. q0 + 15 and blocks p0, p0 + 32 share, ...
+    const int rows16 = rp / 16, share = SMALL_WAVES / rows16, q0 = wave % rows16 * 16, p0 = wave / rows16 * 32;
+    const bool idle = wave >= rows16 * share;
+    auto blocks_of = [&](int columns) { return idle || p0 >= columns ? 0 : (columns - p0 - 1) / (32 * share) + 1; };
+    // acc[i] = the products of all planes for block i of n; the rows of P are columns of the output
+    auto form = [&](floatx4 (&acc)[BLOCKS][2], int n, const char* P, int ppitch, int pplane, auto p_outer, const char* Q, int qpitch, int qplane, int kn) {
+        constexpr bool OUTER = decltype(p_outer)::value;
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) acc[i][0] = acc[i][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+        const uint32_t plane0 = OUTER ? (8 * g + (r >> 2)) * ppitch + 2 * (p0 + 4 * (r & 3)) : (p0 + r) * ppitch + 16 * g;
+        const int next = OUTER ? 64 * share : 32 * share * ppitch, half = OUTER ? 32 : 16 * ppitch, kstep = OUTER ? 32 * ppitch : 64;
+        if (n == 0) return;   // uniform
+        for (int k = 0; k < kn; k += 32) {
+            uint32_t base = plane0 + k / 32 * kstep;
+            asm volatile("" : "+v"(base));   // (each block's address is one addition to this: not kept in registers over the steps)
+            short8v fq[PLANES];
+#pragma unroll
+            for (int z = 0; z < PLANES; ++z) fq[z] = *reinterpret_cast<const short8v*>(Q + z * qplane + (q0 + r) * qpitch + 2 * (k + 8 * g));
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i) {
+                if (i >= n) break;   // uniform
+                short8v fp[PLANES][2];
+#pragma unroll
+                for (int z = 0; z < PLANES; ++z)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        const char* const b = P + z * pplane + i * next + t * half + base;
+                        if constexpr (OUTER) {
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                const short4v h = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(b + 4 * j * ppitch));
+                                fp[z][t][4 * j] = h[0]; fp[z][t][4 * j + 1] = h[1]; fp[z][t][4 * j + 2] = h[2]; fp[z][t][4 * j + 3] = h[3];
+                            }
+                        } else fp[z][t] = *reinterpret_cast<const short8v*>(b);
+                    }
+#pragma unroll
+                for (int sum = PLANES - 1; sum >= 0; --sum)
+#pragma unroll
+                    for (int z = 0; z <= sum; ++z)
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) acc[i][t] = Unit::mfma(fp[z][t], fq[sum - z], acc[i][t]);
+            }
+        }
+    };
+    // four neighbouring values into their planes
+    auto put = [&](char* b, int plane, floatx4 v) {
+#pragma unroll
+        for (int n = 0; n < PLANES; ++n) {
+            short4v h;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint16_t x = to_half(v[e]);
+                h[e] = (short)x;
+                v[e] -= from_half(x);
+            }
+            *reinterpret_cast<short4v*>(b + n * plane) = h;
+        }
+    };
+    auto get = [&](const char* b, int plane) {
+        floatx4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int n = 0; n < PLANES; ++n) {
+            const short4v h = *reinterpret_cast<const short4v*>(b + n * plane);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += from_half((uint16_t)h[e]);
+        }
+        return v;
+    };
+    const int an = blocks_of(rp), xn = blocks_of(cp);
+    const uint32_t aplace = (q0 + r) * apitch + 2 * (p0 + 4 * g), xplace = (q0 + r) * xpitch + 2 * (p0 + 4 * g);   // of this lane's outputs
+    floatx4 out[BLOCKS][2];
+    for (int step = 0; step < a.steps; ++step) {
+        const float ka = a.k[step][0], kb = a.k[step][1], kc = a.k[step][2];
+        // A = X X^T
+        form(out, an, X, xpitch, xplane, Inner(), X, xpitch, xplane, cp);
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+            if (i >= an) break;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) put(A + aplace + 64 * share * i + 32 * t, aplane, out[i][t] * (1.f / ORTHO_SCALE));
+        }
+        __syncthreads();
+        // B = b A + c A^2
+        form(out, an, A, apitch, aplane, Inner(), A, apitch, aplane, rp);
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+            if (i >= an) break;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) out[i][t] = out[i][t] * (kc / ORTHO_SCALE) + get(A + aplace + 64 * share * i + 32 * t, aplane) * kb;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+            if (i >= an) break;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) put(A + aplace + 64 * share * i + 32 * t, aplane, out[i][t]);
+        }
+        __syncthreads();
+        // X <- a X + B X
+        form(out, xn, X, xpitch, xplane, Outer(), A, apitch, aplane, rp);
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+            if (i >= xn) break;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) out[i][t] = out[i][t] * (1.f / ORTHO_SCALE) + get(X + xplace + 64 * share * i + 32 * t, xplane) * ka;
+        }
+        if (step + 1 == a.steps) break;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+            if (i >= xn) break;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) put(X + xplace + 64 * share * i + 32 * t, xplane, out[i][t]);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < BLOCKS; ++i) {
+        if (i >= xn) break;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int row = q0 + r, col = p0 + 32 * share * i + 16 * t + 4 * g + e, gr = m.tall ? col : row, gc = m.tall ? row : col;
+                if (gr < m.rows && gc < m.cols) store_value(m.out, (int64_t)gr * m.cols + gc, m.type, out[i][t][e] * m.out_scale);
+            }
+    }
+}
+
 // ---------------------------------------------------------------- host
 
 static inline int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
@@ -278,6 +507,12 @@ static int ortho_check(const ivfr_orthogonalize_args* a) {
     return IVFR_OK;
 }
 
+#define SMALL_LDS 163584       // (of 163840; the sums of the norm beside it)
+// Whether one workgroup a matrix is the faster way: a compute unit's products against 3 launches a step
+static bool small_pays(const OrthoPlan& p) {
+    return true;
+}
+
 static OrthoPlan ortho_plan(const ivfr_orthogonalize_args& a) {
     OrthoPlan p = {};
     p.tall = a.rows > a.cols;
@@ -295,7 +530,10 @@ static OrthoPlan ortho_plan(const ivfr_orthogonalize_args& a) {
         at += round_up(bytes, 256);
         return here;
     };
-    p.at_sums = take(p.batch * ORTHO_SUMS * 8);
+    p.small = small_lds(p.rp, p.cp, p.planes) <= SMALL_LDS && p.rp <= 128 && small_blocks(p.rp, p.cp) <= SMALL_BLOCKS && small_pays(p);
+    if (p.small) return p;
+    p.parts = (int)std::min<int64_t>(ORTHO_SUMS, (p.xsize + 8191) / 8192);
+    p.at_sums = take(p.batch * p.parts * 8);
     for (int64_t& x : p.at_x) x = take(p.batch * p.planes * p.xsize * 2);
     p.at_a = take(p.batch * p.planes * p.asize * 2);
     p.at_b = take(p.batch * p.planes * p.asize * 2);
@@ -313,7 +551,6 @@ int ivfr_orthogonalize_workspace(const ivfr_orthogonalize_args* args, int64_t* b
 // Tile by the number of them: the largest that gives every compute unit work.
 static int step_tile(int64_t rows, int64_t cols, int64_t batch, int planes, bool triangle) {
     for (int k = planes == 1 ? 0 : IVFR_TILE_128x128; k < IVFR_TILE_64x64; ++k) {
-        if (triangle && k == IVFR_TILE_256x128) continue;
         const int64_t tp = (rows + IVFR_TILE_P[k] - 1) / IVFR_TILE_P[k], tq = (cols + IVFR_TILE_Q[k] - 1) / IVFR_TILE_Q[k];
         if ((triangle ? tp * (tp + 1) / 2 : tp * tq) * batch >= 200) return k;
     }
@@ -347,10 +584,8 @@ static int launch_update_tile(StepArgs a, hipStream_t st) {
 template <int PLANES>
 static int launch_update(const StepArgs& a, hipStream_t st) {
     const int tile = step_tile(a.cp, a.rp, a.batch, PLANES, false);
-    if constexpr (PLANES == 1) {
+    if constexpr (PLANES == 1)
         if (tile == IVFR_TILE_256x256) return launch_update_tile<IVFR_TILE_256x256, 1>(a, st);
-        if (tile == IVFR_TILE_256x128) return launch_update_tile<IVFR_TILE_256x128, 1>(a, st);
-    }
     return tile == IVFR_TILE_128x128 ? launch_update_tile<IVFR_TILE_128x128, PLANES>(a, st) : launch_update_tile<IVFR_TILE_64x64, PLANES>(a, st);
 }
 // one step: A, B, the next X
@@ -371,22 +606,48 @@ static int launch_step(StepArgs s, const float* k, uint16_t* a, uint16_t* b, uin
     return launch_update<PLANES>(s, st);
 }
 
+static int launch_small(const MatrixArgs& m, const ivfr_orthogonalize_args& a, hipStream_t st) {
+    SmallArgs s = {};
+    s.m = m;
+    s.steps = a.steps;
+    for (int i = 0; i < a.steps; ++i)
+        for (int j = 0; j < 3; ++j) s.k[i][j] = a.coefficients[3 * i + j];
+    const dim3 grid((unsigned)a.batch);
+    const bool half = small_lds(m.rp, m.cp, m.planes) <= 81664;   // two workgroups on a compute unit
+    const bool few = small_blocks(m.rp, m.cp) <= 2;
+#define IVFR_SMALL(PLANES, BLOCKS, LDS) hipLaunchKernelGGL((small_kernel<PLANES, BLOCKS, LDS>), grid, dim3(64 * SMALL_WAVES), 0, st, s)
+    if (m.planes == 1) {
+        if (few) IVFR_SMALL(1, 2, 81664);   // (at most 128 x 128)
+        else if (half) IVFR_SMALL(1, SMALL_BLOCKS, 81664);
+        else IVFR_SMALL(1, SMALL_BLOCKS, SMALL_LDS);
+    } else {
+        if (few && half) IVFR_SMALL(2, 2, 81664);
+        else if (few) IVFR_SMALL(2, 2, SMALL_LDS);
+        else IVFR_SMALL(2, SMALL_BLOCKS, SMALL_LDS);
+    }
+#undef IVFR_SMALL
+    IVFR_HIP(hipGetLastError());
+    return IVFR_OK;
+}
+
 int ivfr_orthogonalize(const ivfr_orthogonalize_args* args, void* out, void* workspace, int64_t workspace_bytes, void* stream) {
     IVFR_TRY(ortho_check(args));
     const ivfr_orthogonalize_args& a = *args;
     if (a.batch == 0) return IVFR_OK;
     const OrthoPlan p = ortho_plan(a);
     const int size = a.type == IVFR_TYPE_F32 ? 4 : 2;
-    IVFR_REQUIRE(a.g && out && workspace, "orthogonalize: null pointer");
+    IVFR_REQUIRE(a.g && out && (workspace || p.bytes == 0), "orthogonalize: null pointer");
     IVFR_REQUIRE(((uintptr_t)a.g % size) == 0 && ((uintptr_t)out % size) == 0, "orthogonalize: pointers must be aligned to their type");
     IVFR_REQUIRE(((uintptr_t)workspace & 255) == 0, "orthogonalize: the workspace must be aligned to 256 bytes");
     IVFR_REQUIRE(workspace_bytes >= p.bytes, "orthogonalize: the workspace has %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)p.bytes);
     IVFR_HIP(hipSetDevice(a.device));
     hipStream_t st = (hipStream_t)stream;
     char* const ws = (char*)workspace;
-    MatrixArgs m = {a.g, a.ld, a.batch_stride, a.rows, a.cols, a.type, p.tall, p.rp, p.cp, p.planes, p.xsize, a.eps,
-                    (double*)(ws + p.at_sums), (uint16_t*)(ws + p.at_x[0]), out, a.scale / ORTHO_SCALE};
-    hipLaunchKernelGGL(squares_kernel, dim3(ORTHO_SUMS, (unsigned)p.batch), dim3(256), 0, st, m);
+    MatrixArgs m = {a.g, a.ld, a.batch_stride, a.rows, a.cols, a.type, p.tall, p.rp, p.cp, p.planes, 0, p.xsize, a.eps,
+                    (double*)(ws + p.at_sums), p.parts, (uint16_t*)(ws + p.at_x[0]), out, a.scale / ORTHO_SCALE};
+    m.vec = ((uintptr_t)a.g & 15) == 0 && a.ld * size % 16 == 0 && (a.batch == 1 || a.batch_stride * size % 16 == 0);
+    if (p.small) return launch_small(m, a, st);
+    hipLaunchKernelGGL(squares_kernel, dim3((unsigned)p.parts, (unsigned)p.batch), dim3(256), 0, st, m);
     IVFR_HIP(hipGetLastError());
     const dim3 tiles((unsigned)((p.cp + 63) / 64), (unsigned)((p.rp + 63) / 64), (unsigned)p.batch);
     hipLaunchKernelGGL(fill_kernel, tiles, dim3(256), 0, st, m);

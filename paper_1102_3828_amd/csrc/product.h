@@ -81,20 +81,22 @@ struct Product {
     static_assert(!P_OUTER || BM >= 64, "");
     static_assert(!Q_OUTER || BN >= 64, "");
     static_assert(EACH * (STAGES - 1) < 64 && LDS <= 163840, "");
-    static_assert(PLANES > 1 || KSUB == 1 || KSUB % 2 == 0, "");
+    static_assert(PLANES > 1 || ((KSUB == 1 || KSUB % 2 == 0) && STAGES >= 3), "");
 
     // permutation of the chunks of a row in LDS: inner rows have four of them
     static __device__ __forceinline__ int swz_p(int row) { return ((row >> 1) & 1) | ((row >> 2) & 2); }   // rows 0-3, 8-11 together
     static __device__ __forceinline__ int swz_q(int row) { return (row >> 1) & 3; }                        // rows 0-7 together
-    static __device__ __forceinline__ int swz_k(int k) { return (k & 3) << 1; }                            // four rows of k together
+    // rows of k, of SIZE columns: two lane groups read 32 bytes of four rows each (k..k + 3, k + 8..k + 11) together, from 256 bytes of banks
+    template <int SIZE>
+    static __device__ __forceinline__ int swz_k(int k) { return SIZE == 64 ? (k & 2) | ((k >> 1) & 4) : ((k & 3) << 1) | (k & 8); }
 
     static __device__ __forceinline__ void load16(uint32_t lds, uint32_t offset, const uint16_t* base) {
         // (m0 has the LDS address; the compiler uses it for nothing else here.  No register is written, so none can be taken over early.)
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
     }
-    template <int IN_FLIGHT>
-    static __device__ __forceinline__ void wait_and_meet() {   // all but so many loads of this wavefront are in LDS, its LDS reads are done; then the others' too
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(IN_FLIGHT) : "memory");
+    template <int LOADS, int READS>
+    static __device__ __forceinline__ void wait_and_meet() {   // all but so many loads of this wavefront are in LDS, all but so many of its LDS reads done; then the others' too
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(%1)\n\ts_barrier" ::"n"(LOADS), "n"(READS) : "memory");
     }
     static __device__ __forceinline__ floatx4 mfma(short8v a, short8v b, floatx4 c) {
         if constexpr (HALF) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c, 0, 0, 0);
@@ -111,7 +113,7 @@ struct Product {
         } else {
             constexpr int PER_ROW = SIZE / 8, ROWS = 64 / PER_ROW;
             const int k = ROWS * i + lane / PER_ROW, last = (extent - 1) >> 3;
-            const int chunk = (lane % PER_ROW) ^ swz_k(k);
+            const int chunk = (lane % PER_ROW) ^ swz_k<SIZE>(k);
             return (uint32_t)(k < rows_left ? k : rows_left - 1) * (uint32_t)(2 * ld) + 16u * (chunk < last ? chunk : last);
         }
     }
@@ -122,8 +124,8 @@ struct Product {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
         const int64_t pstep = IVFR_PRODUCT_K * (P_OUTER ? P.ld : 1), qstep = IVFR_PRODUCT_K * (Q_OUTER ? Q.ld : 1);
-        const uint16_t* pn = P.base + (P_OUTER ? (int64_t)p0 : p0 * P.ld) + first * pstep;   // of the next stage to load
-        const uint16_t* qn = Q.base + (Q_OUTER ? (int64_t)q0 : q0 * Q.ld) + first * qstep;
+        const uint16_t* const pn = P.base + (P_OUTER ? (int64_t)p0 : p0 * P.ld) + first * pstep;
+        const uint16_t* const qn = Q.base + (Q_OUTER ? (int64_t)q0 : q0 * Q.ld) + first * qstep;
         uint32_t po[P_KINDS], qo[Q_KINDS];
 #pragma unroll
         for (int i = 0; i < P_KINDS; ++i) po[i] = source<P_OUTER, BM, true>((wave + i * WAVES) % P_ROWS, lane, P.ld, P.extent - p0, IVFR_PRODUCT_K);
@@ -131,29 +133,26 @@ struct Product {
         for (int i = 0; i < Q_KINDS; ++i) qo[i] = source<Q_OUTER, BN, false>((wave + i * WAVES) % Q_ROWS, lane, Q.ld, Q.extent - q0, IVFR_PRODUCT_K);
         const int stages = (count + KSUB - 1) / KSUB;
         int at = 0;   // first slice of the next stage to load
+        // The next stage goes to buffer `buf`.  Past the last slice that one again, so that the number of loads in flight is always the same.
         auto load = [&](int buf) {
             const uint32_t base = lds0 + buf * STAGE;
 #pragma unroll
             for (int i = 0; i < P_EACH; ++i) {
                 const int f = (wave + i * WAVES) % P_LOADS, row = f % P_ROWS, plane = f / P_ROWS % PLANES, sub = f / (P_ROWS * PLANES);
-                const int slice = KSUB == 1 || at + sub < count ? sub : count - 1 - at;   // (past the last one: that again)
-                const int left = P_OUTER ? P.rows - (first + at + slice) * IVFR_PRODUCT_K : IVFR_PRODUCT_K;
-                load16(base + sub * SLICE + plane * P_SLICE + 1024 * row,
-                       P_OUTER && left < IVFR_PRODUCT_K ? source<P_OUTER, BM, true>(row, lane, P.ld, P.extent - p0, left) : po[i % P_KINDS],
-                       pn + slice * pstep + (PLANES > 1 ? plane * P.plane : 0));
+                const int slice = at + sub < count ? at + sub : count - 1;
+                uint32_t o = po[i % P_KINDS];
+                if constexpr (P_OUTER) o = source<true, BM, true>(row, lane, P.ld, P.extent - p0, P.rows - (first + slice) * IVFR_PRODUCT_K);
+                load16(base + sub * SLICE + plane * P_SLICE + 1024 * row, o, pn + slice * pstep + (PLANES > 1 ? plane * P.plane : 0));
             }
 #pragma unroll
             for (int i = 0; i < Q_EACH; ++i) {
                 const int f = (wave + i * WAVES) % Q_LOADS, row = f % Q_ROWS, plane = f / Q_ROWS % PLANES, sub = f / (Q_ROWS * PLANES);
-                const int slice = KSUB == 1 || at + sub < count ? sub : count - 1 - at;
-                const int left = Q_OUTER ? Q.rows - (first + at + slice) * IVFR_PRODUCT_K : IVFR_PRODUCT_K;
-                load16(base + sub * SLICE + PLANES * P_SLICE + plane * Q_SLICE + 1024 * row,
-                       Q_OUTER && left < IVFR_PRODUCT_K ? source<Q_OUTER, BN, false>(row, lane, Q.ld, Q.extent - q0, left) : qo[i % Q_KINDS],
-                       qn + slice * qstep + (PLANES > 1 ? plane * Q.plane : 0));
+                const int slice = at + sub < count ? at + sub : count - 1;
+                uint32_t o = qo[i % Q_KINDS];
+                if constexpr (Q_OUTER) o = source<true, BN, false>(row, lane, Q.ld, Q.extent - q0, Q.rows - (first + slice) * IVFR_PRODUCT_K);
+                load16(base + sub * SLICE + PLANES * P_SLICE + plane * Q_SLICE + 1024 * row, o, qn + slice * qstep + (PLANES > 1 ? plane * Q.plane : 0));
             }
             at += KSUB;
-            pn += KSUB * pstep;
-            qn += KSUB * qstep;
         };
         const int wm = wave / WAVES_N * (BM / WAVES_M), wn = wave % WAVES_N * (BN / WAVES_N);
         const int r = lane & 15, g = lane >> 4;
@@ -166,9 +165,9 @@ struct Product {
             pf[j] = P_OUTER ? k * (2 * BM) : row * KB + 16 * (g ^ swz_p(row));
             qf[j] = Q_OUTER ? k * (2 * BN) : (wn + r) * KB + 16 * (g ^ swz_q(wn + r));
         }
-        auto outer_read = [&](const char* b, const uint32_t (&rows)[2], int column) {   // eight k of column + (l & 15)
+        auto outer_read = [&](const char* b, const uint32_t (&rows)[2], int column, int swizzle) {   // eight k of column + (l & 15)
             short8v v;
-            const int chunk = ((column >> 3) + ((r & 3) >> 1)) ^ swz_k(r >> 2);   // (8 g + 4 j is a multiple of four)
+            const int chunk = ((column >> 3) + ((r & 3) >> 1)) ^ swizzle;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const short4v h = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(b + rows[j] + 16 * chunk + 8 * (r & 1)));
@@ -176,25 +175,16 @@ struct Product {
             }
             return v;
         };
-        auto read = [&](const char* slice, int plane, short8v (&fp)[TM], short8v (&fq)[TN]) {
-            const char* bp = slice + plane * P_SLICE;
-            const char* bq = slice + PLANES * P_SLICE + plane * Q_SLICE;
-#pragma unroll
-            for (int t = 0; t < TN; ++t) {
-                if constexpr (Q_OUTER) fq[t] = outer_read(bq, qf, wn + 16 * t);
-                else fq[t] = *reinterpret_cast<const short8v*>(bq + qf[0] + t * 16 * KB);
-            }
-#pragma unroll
-            for (int t = 0; t < TM; ++t) {
-                if constexpr (P_OUTER) fp[t] = outer_read(bp, pf, wm + 16 * t);
-                else fp[t] = *reinterpret_cast<const short8v*>(bp + pf[t & 1] + (t >> 1) * 32 * KB);
-            }
+        const int pk = swz_k<BM>(8 * g + (r >> 2)), qk = swz_k<BN>(8 * g + (r >> 2));   // (the same four rows further on)
+        auto read_p = [&](const char* slice, int plane, int t) {
+            const char* const b = slice + plane * P_SLICE;
+            if constexpr (P_OUTER) return outer_read(b, pf, wm + 16 * t, pk);
+            else return *reinterpret_cast<const short8v*>(b + pf[t & 1] + (t >> 1) * 32 * KB);
         };
-        auto products = [&](const short8v (&fp)[TM], const short8v (&fq)[TN]) {
-#pragma unroll
-            for (int a = 0; a < TM; ++a)
-#pragma unroll
-                for (int b = 0; b < TN; ++b) acc[a][b] = mfma(fp[a], fq[b], acc[a][b]);
+        auto read_q = [&](const char* slice, int plane, int t) {
+            const char* const b = slice + PLANES * P_SLICE + plane * Q_SLICE;
+            if constexpr (Q_OUTER) return outer_read(b, qf, wn + 16 * t, qk);
+            else return *reinterpret_cast<const short8v*>(b + qf[0] + t * 16 * KB);
         };
 #pragma unroll
         for (int a = 0; a < TM; ++a)
@@ -202,60 +192,85 @@ struct Product {
             for (int b = 0; b < TN; ++b) acc[a][b] = floatx4{0.f, 0.f, 0.f, 0.f};
         if (count <= 0) return;   // uniform
 #pragma unroll
-        for (int s = 0; s < STAGES; ++s)
-            if (s < stages) load(s);
+        for (int s = 0; s < STAGES - 1; ++s) load(s);
         int buf = 0;   // of the stage that is being used
         if constexpr (PLANES == 1) {
-            if (stages >= STAGES) wait_and_meet<(STAGES - 1) * EACH>();
-            else wait_and_meet<0>();
-            short8v fp[2][TM], fq[2][TN];
-            read(smem, 0, fp[0], fq[0]);
-            // slice `sub` of stage s; its fragments are in `c`, those of the next slice go to `n`
-            auto step = [&](int s, int sub, short8v (&cp)[TM], short8v (&cq)[TN], short8v (&np)[TM], short8v (&nq)[TN]) {
-                if (s * KSUB + sub + 1 < count) {
-                    if (sub + 1 < KSUB) read(smem + buf * STAGE + (sub + 1) * SLICE, 0, np, nq);
-                    else {
-                        // loaded are the stages up to s + STAGES - 1; s + 1 is needed, and the buffer of s is free once all have read it
-                        if (s + STAGES - 1 < stages) wait_and_meet<(STAGES - 2) * EACH>();
-                        else wait_and_meet<0>();
-                        if (s + STAGES < stages) load(buf);
-                        buf = buf + 1 == STAGES ? 0 : buf + 1;
-                        read(smem + buf * STAGE, 0, np, nq);
-                    }
-                }
-                products(cp, cq);
-            };
-            if constexpr (KSUB == 1) {
-                for (int s = 0; s < stages; s += 2) {
-                    step(s, 0, fp[0], fq[0], fp[1], fq[1]);
-                    if (s + 1 < stages) step(s + 1, 0, fp[1], fq[1], fp[0], fq[0]);
-                }
-            } else {
-                for (int s = 0; s < stages; ++s)
+            // The fragments of a slice are read during the products of the slice before, each of P in place of the one that has just been used.
+            // At the start of stage s all wavefronts are done with the reads of stage s - 1 (each has at most those of one slice
+            // outstanding, of stage s), so that its buffer is loaded with stage s + STAGES - 1; stages up to s + STAGES - 2 were loaded before, and s + 1 is needed.
+            constexpr int P_READS = P_OUTER ? 2 : 1, Q_READS = Q_OUTER ? 2 : 1, READS = P_READS * TM + Q_READS * TN;
+            short8v fp[TM], fq[2][TN];
+            wait_and_meet<(STAGES - 2) * EACH, 0>();
 #pragma unroll
-                    for (int sub = 0; sub < KSUB; ++sub)
-                        if (s * KSUB + sub < count) step(s, sub, fp[sub & 1], fq[sub & 1], fp[(sub + 1) & 1], fq[(sub + 1) & 1]);
+            for (int t = 0; t < TN; ++t) fq[0][t] = read_q(smem, 0, t);
+#pragma unroll
+            for (int t = 0; t < TM; ++t) fp[t] = read_p(smem, 0, t);
+            // slice number `sub` of its stage
+            auto step = [&](int sub, short8v (&cq)[TN], short8v (&nq)[TN]) {
+                const char* from = smem + buf * STAGE + (sub + 1) * SLICE;
+                if (sub + 1 == KSUB) {
+                    wait_and_meet<(STAGES - 3) * EACH, (READS < 15 ? READS : 15)>();
+                    load(buf == 0 ? STAGES - 1 : buf - 1);
+                    buf = buf + 1 == STAGES ? 0 : buf + 1;
+                    from = smem + buf * STAGE;
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int a = 0; a < TM; ++a) {
+#pragma unroll
+                    for (int b = 0; b < TN; ++b) acc[a][b] = mfma(fp[a], cq[b], acc[a][b]);
+                    fp[a] = read_p(from, 0, a);
+#pragma unroll
+                    for (int b = a * TN / TM; b < (a + 1) * TN / TM; ++b) nq[b] = read_q(from, 0, b);
+                }
+#pragma unroll
+                for (int a = 0; a < TM; ++a) {
+                    __builtin_amdgcn_sched_group_barrier(0x8, TN, 0);
+                    if ((a + 1) * TN / TM > a * TN / TM) __builtin_amdgcn_sched_group_barrier(0x100, P_READS + Q_READS, 0);
+                    else __builtin_amdgcn_sched_group_barrier(0x100, P_READS, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            // (after the last slice the reads bring what nothing uses: the stages past the end hold the last slice again)
+            constexpr int UNROLL = KSUB == 1 ? 2 : KSUB;
+            for (int done = 0;;) {
+#pragma unroll
+                for (int i = 0; i < UNROLL; ++i) {
+                    step(i % KSUB, fq[i & 1], fq[(i + 1) & 1]);
+                    if (++done == count) break;
+                }
+                if (done == count) break;
             }
         } else {
             for (int s = 0; s < stages; ++s) {
-                // loaded are the stages up to s + STAGES - 2 (the first time one more)
-                if (s + STAGES - 2 < stages) wait_and_meet<(STAGES - 2) * EACH>();
-                else wait_and_meet<0>();
-                if (s > 0 && s - 1 + STAGES < stages) load(buf == 0 ? STAGES - 1 : buf - 1);   // (all have read stage s - 1)
+                // loaded are the stages up to s + STAGES - 2
+                wait_and_meet<(STAGES - 2) * EACH, 0>();
+                load(buf == 0 ? STAGES - 1 : buf - 1);   // (all have read stage s - 1)
 #pragma unroll
                 for (int sub = 0; sub < KSUB; ++sub) {
                     if (KSUB > 1 && s * KSUB + sub >= count) break;   // uniform
+                    const char* const from = smem + buf * STAGE + sub * SLICE;
                     short8v fp[PLANES][TM], fq[PLANES][TN];
 #pragma unroll
-                    for (int n = PLANES - 1; n >= 0; --n) read(smem + buf * STAGE + sub * SLICE, n, fp[n], fq[n]);
+                    for (int n = PLANES - 1; n >= 0; --n) {
+#pragma unroll
+                        for (int t = 0; t < TN; ++t) fq[n][t] = read_q(from, n, t);
+#pragma unroll
+                        for (int t = 0; t < TM; ++t) fp[n][t] = read_p(from, n, t);
+                    }
 #pragma unroll
                     for (int sum = PLANES - 1; sum >= 0; --sum)   // small products first
 #pragma unroll
-                        for (int n = 0; n <= sum; ++n) products(fp[n], fq[sum - n]);
+                        for (int n = 0; n <= sum; ++n)
+#pragma unroll
+                            for (int a = 0; a < TM; ++a)
+#pragma unroll
+                                for (int b = 0; b < TN; ++b) acc[a][b] = mfma(fp[n][a], fq[sum - n][b], acc[a][b]);
                 }
                 buf = buf + 1 == STAGES ? 0 : buf + 1;
             }
         }
+        wait_and_meet<0, 0>();   // nothing is on its way to LDS, which may be used for something else from here on
     }
 
     // first p (of four, or with P inner of eight in the tiles t, t + 1) and q of this lane's outputs in tile (t, u)
@@ -269,29 +284,27 @@ struct Product {
     }
 };
 
-// The tiles that there are.  256 x 256 reads least from LDS and memory; of 256 x 128 (and the smaller ones) a compute unit holds two workgroups, so
-// that one forms products while the other starts or ends a tile; the smaller ones are for fewer outputs, the narrow ones for few rows.
+// The tiles that there are.  256 x 256 reads least from LDS and memory per product and is the fastest wherever it gives every compute unit work (scores of 8192 x
+// 131072, d = 2048: 3.6 ms; in tiles of 256 x 128, two workgroups on a compute unit, 4.2; 128 x 128 5.0).  The smaller ones are for fewer outputs, the narrow ones for few rows.
 #define IVFR_TILE_256x256 0
-#define IVFR_TILE_256x128 1
-#define IVFR_TILE_128x128 2
-#define IVFR_TILE_64x64 3
-#define IVFR_TILE_256x64 4
-#define IVFR_TILE_256x16 5
-#define IVFR_TILES 6
-static const int IVFR_TILE_P[IVFR_TILES] = {256, 256, 128, 64, 256, 256}, IVFR_TILE_Q[IVFR_TILES] = {256, 128, 128, 64, 64, 16};
+#define IVFR_TILE_128x128 1
+#define IVFR_TILE_64x64 2
+#define IVFR_TILE_256x64 3
+#define IVFR_TILE_256x16 4
+#define IVFR_TILES 5
+static const int IVFR_TILE_P[IVFR_TILES] = {256, 128, 64, 256, 256}, IVFR_TILE_Q[IVFR_TILES] = {256, 128, 64, 64, 16};
 template <int TILE, bool PO, bool QO, bool HALF, int PLANES> struct ProductOf;
 template <bool PO, bool QO, bool HALF> struct ProductOf<0, PO, QO, HALF, 1> { typedef Product<256, 256, 2, 4, PO, QO, HALF, 1, 1, 4> T; };
-template <bool PO, bool QO, bool HALF> struct ProductOf<1, PO, QO, HALF, 1> { typedef Product<256, 128, 2, 2, PO, QO, HALF, 1, 1, 3> T; };
-template <bool PO, bool QO, bool HALF> struct ProductOf<2, PO, QO, HALF, 1> { typedef Product<128, 128, 2, 2, PO, QO, HALF, 1, 1, 4> T; };
-template <bool PO, bool QO, bool HALF> struct ProductOf<3, PO, QO, HALF, 1> { typedef Product<64, 64, 2, 2, PO, QO, HALF, 1, 2, 4> T; };
-template <bool PO, bool QO, bool HALF> struct ProductOf<4, PO, QO, HALF, 1> { typedef Product<256, 64, 8, 1, PO, QO, HALF, 1, 1, 4> T; };
-template <bool PO, bool QO, bool HALF> struct ProductOf<5, PO, QO, HALF, 1> { typedef Product<256, 16, 8, 1, PO, QO, HALF, 1, 1, 4> T; };
-template <bool PO, bool QO, bool HALF> struct ProductOf<2, PO, QO, HALF, 2> { typedef Product<128, 128, 2, 4, PO, QO, HALF, 2, 1, 4> T; };
-template <bool PO, bool QO, bool HALF> struct ProductOf<3, PO, QO, HALF, 2> { typedef Product<64, 64, 2, 2, PO, QO, HALF, 2, 1, 4> T; };
-template <bool PO, bool QO, bool HALF> struct ProductOf<2, PO, QO, HALF, 3> { typedef Product<128, 128, 2, 4, PO, QO, HALF, 3, 1, 3> T; };
-template <bool PO, bool QO, bool HALF> struct ProductOf<3, PO, QO, HALF, 3> { typedef Product<64, 64, 2, 2, PO, QO, HALF, 3, 1, 3> T; };
-template <bool PO, bool QO, bool HALF> struct ProductOf<4, PO, QO, HALF, 3> { typedef Product<256, 64, 8, 1, PO, QO, HALF, 3, 1, 2> T; };
-template <bool PO, bool QO, bool HALF> struct ProductOf<5, PO, QO, HALF, 3> { typedef Product<256, 16, 8, 1, PO, QO, HALF, 3, 1, 3> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<1, PO, QO, HALF, 1> { typedef Product<128, 128, 2, 2, PO, QO, HALF, 1, 1, 4> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<2, PO, QO, HALF, 1> { typedef Product<64, 64, 2, 2, PO, QO, HALF, 1, 2, 4> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<3, PO, QO, HALF, 1> { typedef Product<256, 64, 8, 1, PO, QO, HALF, 1, 1, 4> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<4, PO, QO, HALF, 1> { typedef Product<256, 16, 8, 1, PO, QO, HALF, 1, 1, 4> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<1, PO, QO, HALF, 2> { typedef Product<128, 128, 2, 4, PO, QO, HALF, 2, 1, 4> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<2, PO, QO, HALF, 2> { typedef Product<64, 64, 2, 2, PO, QO, HALF, 2, 1, 4> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<1, PO, QO, HALF, 3> { typedef Product<128, 128, 2, 4, PO, QO, HALF, 3, 1, 3> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<2, PO, QO, HALF, 3> { typedef Product<64, 64, 2, 2, PO, QO, HALF, 3, 1, 3> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<3, PO, QO, HALF, 3> { typedef Product<256, 64, 8, 1, PO, QO, HALF, 3, 1, 2> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<4, PO, QO, HALF, 3> { typedef Product<256, 16, 8, 1, PO, QO, HALF, 3, 1, 3> T; };
 
 // rounding to nearest, ties to even
 __device__ __forceinline__ uint16_t to_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }

@@ -98,14 +98,14 @@ struct TileCost {
     int resident[3];
     double slice[3];
 };
-static const TileCost COSTS[IVFR_TILES] = {{{1, 0, 0}, {1600, 0, 0}}, {{2, 0, 0}, {1700, 0, 0}}, {{2, 1, 1}, {1000, 1500, 2600}},
+static const TileCost COSTS[IVFR_TILES] = {{{1, 0, 0}, {1600, 0, 0}}, {{2, 1, 1}, {1000, 1500, 2600}},
                                            {{2, 2, 2}, {320, 700, 1200}}, {{0, 0, 0}, {0, 0, 0}}, {{2, 0, 1}, {420, 0, 900}}};
 
 void product_cut(int64_t np, int64_t nq, int64_t slices, int planes, bool q_outer, int* tile, int* splits) {
     double least = 1e300;
     for (int k = 0; k < IVFR_TILES; ++k) {
         const int resident = COSTS[k].resident[planes - 1];
-        if (!resident || (k == IVFR_TILE_256x16 && (q_outer || nq > 64)) || (k == IVFR_TILE_256x128 && q_outer)) continue;   // (256 x 128 with both outer: out of registers)
+        if (!resident || (k == IVFR_TILE_256x16 && (q_outer || nq > 64))) continue;
         const int64_t tiles = ((np + IVFR_TILE_P[k] - 1) / IVFR_TILE_P[k]) * ((nq + IVFR_TILE_Q[k] - 1) / IVFR_TILE_Q[k]);
         for (int s = 1; s <= 128 && s <= slices; s *= 2) {
             const int64_t per = (slices + s - 1) / s, parts = (slices + per - 1) / per, slots = (int64_t)IVFR_PRODUCT_CU * resident;
@@ -137,16 +137,13 @@ static int launch_one(const ProductOut& o, hipStream_t st) {
 template <bool QO, bool HALF, int PLANES>
 static int launch_tile(const ProductOut& o, hipStream_t st) {
     switch (o.tile) {
-        case 2: return launch_one<2, QO, HALF, PLANES>(o, st);
-        case 3: return launch_one<3, QO, HALF, PLANES>(o, st);
-        case 5:
-            if constexpr (!QO) return launch_one<5, false, HALF, PLANES>(o, st);
+        case IVFR_TILE_256x256:
+            if constexpr (PLANES == 1) return launch_one<IVFR_TILE_256x256, QO, HALF, 1>(o, st);
             break;
-        case 0:
-            if constexpr (PLANES == 1) return launch_one<0, QO, HALF, 1>(o, st);
-            break;
-        case 1:
-            if constexpr (PLANES == 1 && !QO) return launch_one<1, false, HALF, 1>(o, st);
+        case IVFR_TILE_128x128: return launch_one<IVFR_TILE_128x128, QO, HALF, PLANES>(o, st);
+        case IVFR_TILE_64x64: return launch_one<IVFR_TILE_64x64, QO, HALF, PLANES>(o, st);
+        case IVFR_TILE_256x16:
+            if constexpr (!QO) return launch_one<IVFR_TILE_256x16, false, HALF, PLANES>(o, st);
             break;
     }
     ivfr_set_error("no such tile of a product: %d", o.tile);
@@ -163,8 +160,8 @@ static int launch_two(const ProductOut& x, const ProductOut& w, hipStream_t st) 
 }
 template <bool HALF, int PLANES>
 static int launch_both(const ProductOut& x, const ProductOut& w, hipStream_t st) {
-    if (x.tile == w.tile && x.tile == IVFR_TILE_128x128) return launch_two<2, HALF, PLANES>(x, w, st);
-    if (x.tile == w.tile && x.tile == IVFR_TILE_64x64) return launch_two<3, HALF, PLANES>(x, w, st);
+    if (x.tile == w.tile && x.tile == IVFR_TILE_128x128) return launch_two<IVFR_TILE_128x128, HALF, PLANES>(x, w, st);
+    if (x.tile == w.tile && x.tile == IVFR_TILE_64x64) return launch_two<IVFR_TILE_64x64, HALF, PLANES>(x, w, st);
     IVFR_TRY((launch_tile<false, HALF, PLANES>(x, st)));
     return launch_tile<true, HALF, PLANES>(w, st);
 }

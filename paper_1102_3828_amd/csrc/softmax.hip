@@ -137,12 +137,12 @@ struct ScoreArgs {
 
 // scores of this lane's outputs times log2 e (exponentials are powers of two from here on), in place; vectors that take no part, or do not exist: -inf
 template <class C>
-__device__ __forceinline__ void scores(const ScoreArgs& a, int p0, floatx4 (&acc)[C::TM][C::TN]) {
-    if (!a.offset && p0 + C::BM <= a.v) {   // uniform
+__device__ __forceinline__ void scores(float scale, const float* offset, int v, int p0, floatx4 (&acc)[C::TM][C::TN]) {
+    if (!offset && p0 + C::BM <= v) {   // uniform
 #pragma unroll
         for (int t = 0; t < C::TM; ++t)
 #pragma unroll
-            for (int u = 0; u < C::TN; ++u) acc[t][u] *= a.scale;
+            for (int u = 0; u < C::TN; ++u) acc[t][u] *= scale;
         return;
     }
 #pragma unroll
@@ -150,24 +150,19 @@ __device__ __forceinline__ void scores(const ScoreArgs& a, int p0, floatx4 (&acc
         const int j = p0 + C::p_of(t);
         float o[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) o[r] = j + r < a.v ? (a.offset ? a.offset[j + r] * LOG2E : 0.f) : -INFINITY;
+        for (int r = 0; r < 4; ++r) o[r] = j + r < v ? (offset ? offset[j + r] * LOG2E : 0.f) : -INFINITY;
 #pragma unroll
         for (int u = 0; u < C::TN; ++u)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) acc[t][u][r] = o[r] == -INFINITY ? -INFINITY : fmaf(acc[t][u][r], a.scale, o[r]);
+            for (int r = 0; r < 4; ++r) acc[t][u][r] = o[r] == -INFINITY ? -INFINITY : fmaf(acc[t][u][r], scale, o[r]);
     }
 }
 
-// value = f(value) for the output at row `at` of the tile (negative: none) in column u, by the lane that has it.
-template <class C, class F>
-__device__ __forceinline__ void at_row(floatx4 (&acc)[C::TM][C::TN], int u, int at, F f) {
+// Which of this lane's outputs (4 t + r) of a column is at row `at` of the tile; negative if none is.
+template <class C>
+__device__ __forceinline__ int output_at(int at) {
     const int lane = threadIdx.x & 63, rel = at - (int)(threadIdx.x >> 6) / C::WAVES_N * (C::BM / C::WAVES_M);
-    if (at < 0 || rel < 0 || rel >= C::BM / C::WAVES_M || ((rel >> 3) & 3) != lane >> 4) return;
-#pragma unroll
-    for (int t = 0; t < C::TM; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if ((rel >> 5) * 2 + ((rel >> 2) & 1) == t && (rel & 3) == r) acc[t][u][r] = f(acc[t][u][r]);
+    return at < 0 || rel < 0 || rel >= C::BM / C::WAVES_M || ((rel >> 3) & 3) != lane >> 4 ? -1 : (rel >> 5) * 8 + (rel & 7);
 }
 
 template <class C>
@@ -178,7 +173,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void score_kernel(ScoreA
     const int p0 = tile.p * C::BM, q0 = tile.q * C::BN;
     floatx4 acc[C::TM][C::TN];
     C::run(a.w, a.x, p0, q0, 0, a.slices, smem, acc);
-    scores<C>(a, p0, acc);
+    scores<C>(a.scale, a.offset, a.v, p0, acc);
     __syncthreads();   // the stages are no longer read
     float2* const red = reinterpret_cast<float2*>(smem);   // [WAVES_M][BN]
     const int lane = threadIdx.x & 63, wm = (threadIdx.x >> 6) / C::WAVES_N;
@@ -186,7 +181,18 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void score_kernel(ScoreA
     for (int u = 0; u < C::TN; ++u) {
         const int i = q0 + C::q_of(u);
         const int64_t target = i < a.n ? a.targets[i] : -1;
-        at_row<C>(acc, u, target >= p0 && target < a.v && target < p0 + C::BM ? (int)target - p0 : -1, [&](float z) { return a.target_score[i] = z; });   // (one lane of the launch)
+        const int own = output_at<C>(target >= p0 && target < a.v && target < p0 + C::BM ? (int)target - p0 : -1);
+        if (own >= 0) {   // one lane of the launch
+            float z = 0.f;
+#pragma unroll
+            for (int t = 0; t < C::TM; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {   // (selects: an index that varies would put the outputs into memory)
+                    const float x = acc[t][u][r];
+                    if (own == 4 * t + r) z = x;
+                }
+            a.target_score[i] = z;
+        }
         float m = -INFINITY;
 #pragma unroll
         for (int t = 0; t < C::TM; ++t)
@@ -266,7 +272,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void grad_score_kernel(S
     const int p0 = tile.p * C::BM, q0 = tile.q * C::BN;
     floatx4 acc[C::TM][C::TN];
     C::run(a.w, a.x, p0, q0, 0, a.slices, smem, acc);
-    scores<C>(a, p0, acc);
+    scores<C>(a.scale, a.offset, a.v, p0, acc);
     const float unit = a.unit ? a.unit[0] : 1.f;
 #pragma unroll
     for (int u = 0; u < C::TN; ++u) {
@@ -288,7 +294,13 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void grad_score_kernel(S
         {   // the row's own vector, if it is in this tile and takes part: p - 1 before anything is rounded
             int at = target >= (int64_t)a.v0 + p0 && target < (int64_t)a.v0 + a.v && target < (int64_t)a.v0 + p0 + C::BM ? (int)(target - a.v0 - p0) : -1;
             if (at >= 0 && a.offset && a.offset[p0 + at] == -INFINITY) at = -1;
-            at_row<C>(acc, u, at, [](float p) { return p - 1.f; });
+            const int own = output_at<C>(at);
+            if (own >= 0) {
+#pragma unroll
+                for (int t = 0; t < C::TM; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[t][u][r] -= own == 4 * t + r ? 1.f : 0.f;
+            }
         }
         const bool live = g != 0.f;   // (a row without gradient: zeros, whatever its statistics are)
 #pragma unroll
@@ -324,7 +336,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void grad_score_kernel(S
 static int score_tile(int64_t n, int64_t v, int planes) {
     if (n <= 16) return IVFR_TILE_256x16;
     if (n <= 64) return IVFR_TILE_256x64;
-    if (planes == 1 && ((n + 127) / 128) * ((v + 255) / 256) >= IVFR_PRODUCT_CU) return IVFR_TILE_256x128;
+    if (planes == 1 && ((n + 255) / 256) * ((v + 255) / 256) >= IVFR_PRODUCT_CU * 3 / 4) return IVFR_TILE_256x256;
     return ((n + 127) / 128) * ((v + 127) / 128) >= IVFR_PRODUCT_CU / 2 ? IVFR_TILE_128x128 : IVFR_TILE_64x64;
 }
 
@@ -340,8 +352,8 @@ static int launch_score_tile(const ScoreArgs& a, bool grad, hipStream_t st) {
 template <bool HALF, int PLANES>
 static int launch_score_planes(const ScoreArgs& a, int tile, bool grad, hipStream_t st) {
     switch (tile) {
-        case IVFR_TILE_256x128:
-            if constexpr (PLANES == 1) return launch_score_tile<IVFR_TILE_256x128, HALF, 1>(a, grad, st);
+        case IVFR_TILE_256x256:
+            if constexpr (PLANES == 1) return launch_score_tile<IVFR_TILE_256x256, HALF, 1>(a, grad, st);
             break;
         case IVFR_TILE_128x128: return launch_score_tile<IVFR_TILE_128x128, HALF, PLANES>(a, grad, st);
         case IVFR_TILE_64x64: return launch_score_tile<IVFR_TILE_64x64, HALF, PLANES>(a, grad, st);
