@@ -19,7 +19,7 @@
 #define ORTHO_SUMS 256         // workgroups at most that sum the squares of a matrix
 
 struct OrthoPlan {
-    int r, c, rp, cp, planes;
+    int r, c, rp, cp, xld, ald, planes;
     bool tall, small;
     int64_t batch;
     int parts;
@@ -31,7 +31,7 @@ struct MatrixArgs {
     const void* g;
     int64_t ld, batch_stride;
     int rows, cols, type;      // of g
-    int tall, rp, cp, planes, vec;   // vec: rows start at 16-byte boundaries
+    int tall, rp, cp, xld, planes, vec;   // vec: rows start at 16-byte boundaries
     int64_t xsize;             // elements of a plane; a matrix has `planes` of them
     float eps;
     double* sums;              // [batch][parts]
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(256) void fill_kernel(MatrixArgs a) {
         const int row = r0 + i, col = c0 + lane;
         if (row >= a.rp || col >= a.cp) continue;
         const float v = a.tall ? tile[i][lane] : (row < r && col < c ? (float)(load_value(a.g, base + (int64_t)row * a.ld + col, a.type) * inv) : 0.f);
-        store_planes(x + (int64_t)row * a.cp + col, a.xsize, a.planes, v);
+        store_planes(x + (int64_t)row * a.xld + col, a.xsize, a.planes, v);
     }
 }
 
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(256) void emit_kernel(MatrixArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int i = wave; i < 64; i += 4) {
         const int row = r0 + i, col = c0 + lane;
-        tile[lane][i] = row < a.rp && col < a.cp ? load_planes(x + (int64_t)row * a.cp + col, a.xsize, a.planes) : 0.f;
+        tile[lane][i] = row < a.rp && col < a.cp ? load_planes(x + (int64_t)row * a.xld + col, a.xsize, a.planes) : 0.f;
     }
     __syncthreads();
     for (int i = wave; i < 64; i += 4) {
@@ -150,7 +150,7 @@ struct StepArgs {
     const uint16_t *x, *in;    // X of the step; A (forming B), B (forming X)
     uint16_t* y;               // A, B or the next X
     int64_t xsize, asize;
-    int rp, cp, planes;
+    int rp, cp, xld, ald, planes;
     int tiles_p, tiles_q, batch;
     float first, second;       // of what is added, of the product
     // of the last step of a matrix that is not tall: the result
@@ -173,30 +173,34 @@ template <class C, bool SQUARE>
 __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void gram_kernel(StepArgs a) {
     __shared__ __align__(1024) char smem[C::LDS];
     const uint32_t each = (uint32_t)a.tiles_p * (a.tiles_p + 1) / 2, total = each * (uint32_t)a.batch, per = (total + 7) / 8;
-    const uint32_t id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if ((blockIdx.x >> 3) >= per || id >= total) return;   // uniform
-    const uint32_t m = (uint32_t)__builtin_amdgcn_readfirstlane((int)(id / each));
-    int tp, tq;
-    triangle(id - m * each, tp, tq);
-    const int p0 = tp * C::BM, q0 = tq * C::BN;
     const int64_t size = SQUARE ? a.asize : a.xsize;
-    const uint16_t* const src = (SQUARE ? a.in : a.x) + (int64_t)m * a.planes * size;
-    const ProductOperand o = {src, size, SQUARE ? a.rp : a.cp, a.rp, 0};
-    floatx4 acc[C::TM][C::TN];
-    C::run(o, o, p0, q0, 0, (SQUARE ? a.rp : a.cp) / IVFR_PRODUCT_K, smem, acc);
-    uint16_t* const y = a.y + (int64_t)m * a.planes * a.asize;
+    const uint16_t* const src0 = SQUARE ? a.in : a.x;
+    const ProductOperand operand = {src0, size, SQUARE ? a.ald : a.xld, a.rp, 0};
+    C::run(operand, operand, smem, [&](uint32_t i, ProductWork& w) {
+        const uint32_t local = (blockIdx.x >> 3) + i * (gridDim.x >> 3), id = (blockIdx.x & 7) * per + local;
+        if (local >= per || id >= total) return false;
+        w.split = __builtin_amdgcn_readfirstlane((int)(id / each));
+        triangle(id - w.split * each, w.p, w.q);
+        w.first = 0;
+        w.count = (SQUARE ? a.rp : a.cp) / IVFR_PRODUCT_K;
+        w.p_at = w.q_at = (int64_t)w.split * a.planes * size;
+        return true;
+    }, [&](const ProductWork& tile, floatx4 (&acc)[C::TM][C::TN]) {
+    const int tid = C::thread(), tp = tile.p, tq = tile.q, p0 = tp * C::BM, q0 = tq * C::BN;
+    const uint16_t* const src = src0 + tile.p_at;
+    uint16_t* const y = a.y + (int64_t)tile.split * a.planes * a.asize;
 #pragma unroll
     for (int u = 0; u < C::TN; ++u) {
-        const int q = q0 + C::q_of(u);
+        const int q = q0 + C::q_of(tid, u);
         if (q >= a.rp) continue;
 #pragma unroll
         for (int t = 0; t < C::TM; t += 2) {
-            const int p = p0 + C::p_of(t);
+            const int p = p0 + C::p_of(tid, t);
             if (p >= a.rp) continue;   // (a multiple of 8, as p)
             float v[8];
 #pragma unroll
             for (int r = 0; r < 8; ++r) v[r] = a.second * acc[t + (r >> 2)][u][r & 3];
-            const int64_t at = (int64_t)q * a.rp + p;
+            const int64_t at = (int64_t)q * a.ald + p;
             if constexpr (SQUARE) {
                 const half8v h = *reinterpret_cast<const half8v*>(src + at);
                 half8v l = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -213,12 +217,12 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void gram_kernel(StepArg
                     const uint16_t b = to_half(v[r]);
                     h[r] = (short)b;
                     v[r] -= from_half(b);
-                    if (tp != tq) o[(int64_t)(p + r) * a.rp + q] = b;
+                    if (tp != tq) o[(int64_t)(p + r) * a.ald + q] = b;
                 }
                 *reinterpret_cast<short8v*>(o + at) = h;
             }
         }
-    }
+    }    });
 }
 
 typedef _Float16 half4v __attribute__((ext_vector_type(4)));
@@ -227,23 +231,27 @@ typedef _Float16 half4v __attribute__((ext_vector_type(4)));
 template <class C>
 __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void update_kernel(StepArgs a) {
     __shared__ __align__(1024) char smem[C::LDS];
-    const ProductTile tile = product_tile(blockIdx.x, a.tiles_p, a.tiles_q, a.batch);
-    if (!tile.any) return;   // uniform
-    const int p0 = tile.p * C::BM, q0 = tile.q * C::BN;
-    const uint16_t* const x = a.x + (int64_t)tile.split * a.planes * a.xsize;
-    const ProductOperand P = {x, a.xsize, a.cp, a.cp, a.rp}, Q = {a.in + (int64_t)tile.split * a.planes * a.asize, a.asize, a.rp, a.rp, 0};
-    floatx4 acc[C::TM][C::TN];
-    C::run(P, Q, p0, q0, 0, a.rp / IVFR_PRODUCT_K, smem, acc);
-    uint16_t* const y = a.y + (int64_t)tile.split * a.planes * a.xsize;
+    const ProductOperand P = {a.x, a.xsize, a.xld, a.cp, a.rp}, Q = {a.in, a.asize, a.ald, a.rp, 0};
+    C::run(P, Q, smem, [&](uint32_t i, ProductWork& w) {
+        if (!product_work(i, blockIdx.x, gridDim.x, a.tiles_p, a.tiles_q, a.batch, w)) return false;
+        w.first = 0;
+        w.count = a.rp / IVFR_PRODUCT_K;
+        w.p_at = (int64_t)w.split * a.planes * a.xsize;
+        w.q_at = (int64_t)w.split * a.planes * a.asize;
+        return true;
+    }, [&](const ProductWork& tile, floatx4 (&acc)[C::TM][C::TN]) {
+    const int tid = C::thread(), p0 = tile.p * C::BM, q0 = tile.q * C::BN;
+    const uint16_t* const x = a.x + tile.p_at;
+    uint16_t* const y = a.y + tile.p_at;
 #pragma unroll
     for (int u = 0; u < C::TN; ++u) {
-        const int q = q0 + C::q_of(u);
+        const int q = q0 + C::q_of(tid, u);
         if (q >= a.rp) continue;
 #pragma unroll
         for (int t = 0; t < C::TM; ++t) {
-            const int p = p0 + C::p_of(t);
+            const int p = p0 + C::p_of(tid, t);
             if (p >= a.cp) continue;   // (a multiple of 4, as p)
-            const int64_t at = (int64_t)q * a.cp + p;
+            const int64_t at = (int64_t)q * a.xld + p;
             const half4v h = *reinterpret_cast<const half4v*>(x + at);
             half4v l = {0, 0, 0, 0};
             if (a.planes > 1) l = *reinterpret_cast<const half4v*>(x + a.xsize + at);
@@ -268,7 +276,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void update_kernel(StepA
                 }
             }
         }
-    }
+    }    });
 }
 
 // ---------------------------------------------------------------- small matrices
@@ -522,8 +530,10 @@ static OrthoPlan ortho_plan(const ivfr_orthogonalize_args& a) {
     p.cp = (int)round_up(p.c, 32);
     p.planes = a.type == IVFR_TYPE_F32 ? 2 : 1;
     p.batch = a.batch;
-    p.xsize = (int64_t)p.rp * p.cp;
-    p.asize = (int64_t)p.rp * p.rp;
+    p.xld = (int)product_ld(p.cp);
+    p.ald = (int)product_ld(p.rp);
+    p.xsize = (int64_t)p.rp * p.xld;
+    p.asize = (int64_t)p.rp * p.ald;
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
         const int64_t here = at;
@@ -561,7 +571,7 @@ template <int TILE, int PLANES, bool SQUARE>
 static int launch_gram_tile(StepArgs a, hipStream_t st) {
     typedef typename ProductOf<TILE, false, false, true, PLANES>::T C;
     a.tiles_p = (a.rp + C::BM - 1) / C::BM;
-    hipLaunchKernelGGL((gram_kernel<C, SQUARE>), dim3(product_grid((int64_t)a.tiles_p * (a.tiles_p + 1) / 2 * a.batch)), dim3(C::THREADS), 0, st, a);
+    hipLaunchKernelGGL((gram_kernel<C, SQUARE>), dim3(product_grid((int64_t)a.tiles_p * (a.tiles_p + 1) / 2 * a.batch, C::RESIDENT)), dim3(C::THREADS), 0, st, a);
     IVFR_HIP(hipGetLastError());
     return IVFR_OK;
 }
@@ -577,7 +587,7 @@ static int launch_update_tile(StepArgs a, hipStream_t st) {
     typedef typename ProductOf<TILE, true, false, true, PLANES>::T C;
     a.tiles_p = (a.cp + C::BM - 1) / C::BM;
     a.tiles_q = (a.rp + C::BN - 1) / C::BN;
-    hipLaunchKernelGGL((update_kernel<C>), dim3(product_grid((int64_t)a.tiles_p * a.tiles_q * a.batch)), dim3(C::THREADS), 0, st, a);
+    hipLaunchKernelGGL((update_kernel<C>), dim3(product_grid((int64_t)a.tiles_p * a.tiles_q * a.batch, C::RESIDENT)), dim3(C::THREADS), 0, st, a);
     IVFR_HIP(hipGetLastError());
     return IVFR_OK;
 }
@@ -643,7 +653,7 @@ int ivfr_orthogonalize(const ivfr_orthogonalize_args* args, void* out, void* wor
     IVFR_HIP(hipSetDevice(a.device));
     hipStream_t st = (hipStream_t)stream;
     char* const ws = (char*)workspace;
-    MatrixArgs m = {a.g, a.ld, a.batch_stride, a.rows, a.cols, a.type, p.tall, p.rp, p.cp, p.planes, 0, p.xsize, a.eps,
+    MatrixArgs m = {a.g, a.ld, a.batch_stride, a.rows, a.cols, a.type, p.tall, p.rp, p.cp, p.xld, p.planes, 0, p.xsize, a.eps,
                     (double*)(ws + p.at_sums), p.parts, (uint16_t*)(ws + p.at_x[0]), out, a.scale / ORTHO_SCALE};
     m.vec = ((uintptr_t)a.g & 15) == 0 && a.ld * size % 16 == 0 && (a.batch == 1 || a.batch_stride * size % 16 == 0);
     if (p.small) return launch_small(m, a, st);
@@ -657,6 +667,8 @@ int ivfr_orthogonalize(const ivfr_orthogonalize_args* args, void* out, void* wor
     s.asize = p.asize;
     s.rp = p.rp;
     s.cp = p.cp;
+    s.xld = p.xld;
+    s.ald = p.ald;
     s.planes = p.planes;
     s.batch = (int)p.batch;
     s.rows = a.rows;

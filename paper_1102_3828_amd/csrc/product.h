@@ -16,6 +16,8 @@
 
 #include "ivfr_internal.h"
 
+#include <algorithm>
+
 typedef short short4v __attribute__((ext_vector_type(4)));
 typedef short short8v __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
@@ -31,29 +33,36 @@ struct ProductOperand {
     int64_t ld;             // elements between rows, a multiple of 8
     int extent;             // values of the operand's own index; beyond it the last one (inner), or its last chunk of eight (outer), is read again
     int rows;               // outer: rows of k that may be read; beyond them the last one is read again
+    // Elements between panels of 256 of the inner axis.  256: rows lie whole.  A matrix kept in panels (ld 256) has its tiles in one piece each, where whole
+    // rows of a hundred KB would spread a tile over as many pages as it has rows.
+    int64_t panel = 256;
 };
+// Elements between the rows of an operand that is laid out here: whole lines of 128 bytes (with rows that begin inside a line every stage reads lines by halves: 8 % more time)
+inline int64_t product_ld(int64_t k) { return (k + 63) / 64 * 64; }
 
-// What a workgroup computes of a launch's tiles: XCDs take contiguous runs of them (blocks go round the eight XCDs, each with an L2 of its
-// own), and a run walks over patches of eight tiles of p.
-struct ProductTile {
-    int p, q, split;
-    bool any;
+// What a workgroup computes of a launch's tiles: the i-th tile of workgroup `block` of `blocks`.  XCDs take contiguous runs of tiles (blocks go round the
+// eight XCDs, each with an L2 of its own), and a run walks over patches of eight tiles of p.
+struct ProductWork {
+    int p, q, split;       // the tile
+    int first, count;      // its slices of k
+    int64_t p_at, q_at;    // elements from the operands' bases (a matrix of a batch)
 };
-__device__ __forceinline__ ProductTile product_tile(uint32_t block, int tiles_p, int tiles_q, int splits) {
+__device__ __forceinline__ bool product_work(uint32_t i, uint32_t block, uint32_t blocks, int tiles_p, int tiles_q, int splits, ProductWork& w) {
     const uint32_t total = (uint32_t)tiles_p * (uint32_t)tiles_q * (uint32_t)splits, per = (total + 7) / 8;
-    const uint32_t id = (block & 7) * per + (block >> 3);
-    ProductTile t = {0, 0, 0, (block >> 3) < per && id < total};
+    const uint32_t local = (block >> 3) + i * (blocks >> 3), id = (block & 7) * per + local;
+    if (local >= per || id >= total) return false;
     const uint32_t each = (uint32_t)tiles_p * (uint32_t)tiles_q;
     const uint32_t split = id / each;
     const uint32_t in = id - split * each, band = 8u * (uint32_t)tiles_q, b = in / band, first = 8 * b;
     const uint32_t high = (uint32_t)tiles_p - first < 8u ? (uint32_t)tiles_p - first : 8u;
     // (uniform, but divisions are formed in vector registers, and the addresses made of these have to be in scalar ones)
-    t.split = __builtin_amdgcn_readfirstlane((int)split);
-    t.p = __builtin_amdgcn_readfirstlane((int)(first + (in - b * band) % high));
-    t.q = __builtin_amdgcn_readfirstlane((int)((in - b * band) / high));
-    return t;
+    w.split = __builtin_amdgcn_readfirstlane((int)split);
+    w.p = __builtin_amdgcn_readfirstlane((int)(first + (in - b * band) % high));
+    w.q = __builtin_amdgcn_readfirstlane((int)((in - b * band) / high));
+    return true;
 }
-inline unsigned product_grid(int64_t tiles) { return (unsigned)((tiles + 7) / 8 * 8); }
+// workgroups of a launch: no more than the compute units hold; a workgroup goes on with its next tile
+inline unsigned product_grid(int64_t tiles, int resident) { return (unsigned)std::min<int64_t>((tiles + 7) / 8 * 8, (int64_t)IVFR_PRODUCT_CU * resident); }
 
 // PLANES of fp32 operands: 3 of bf16 (24 bits), of which the six products with a + b <= 2 are formed (what they neglect is 2^-24 of the whole), or 2 of
 // fp16 (22 bits and a sign), three products (2^-22).  All planes of a stage's k are in LDS at once.
@@ -118,39 +127,60 @@ struct Product {
         }
     }
 
-    // The accumulators of one tile over the slices [first, first + count).  p0, q0: the tile's first p and q, below the operands' extents.
-    static __device__ __forceinline__ void run(const ProductOperand& P, const ProductOperand& Q, int p0, int q0, int first, int count, char* smem,
-                                               floatx4 (&acc)[TM][TN]) {
+    // All tiles of this workgroup.  work(i, w): its i-th tile, false if there is none; done(w, acc): the sums of tile w, in all wavefronts about the same time.
+    // Stages of the next tile are loaded, and its first fragments read, while the last slices of a tile are used and its sums are dealt with.
+    template <class Work, class Done>
+    static __device__ __forceinline__ void run(const ProductOperand& P, const ProductOperand& Q, char* smem, Work work, Done done) {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-        const int64_t pstep = IVFR_PRODUCT_K * (P_OUTER ? P.ld : 1), qstep = IVFR_PRODUCT_K * (Q_OUTER ? Q.ld : 1);
-        const uint16_t* const pn = P.base + (P_OUTER ? (int64_t)p0 : p0 * P.ld) + first * pstep;
-        const uint16_t* const qn = Q.base + (Q_OUTER ? (int64_t)q0 : q0 * Q.ld) + first * qstep;
+        auto slice_at = [](const ProductOperand& o, bool outer, int slice) { return outer ? slice * (IVFR_PRODUCT_K * o.ld) : (slice >> 3) * o.panel + (slice & 7) * IVFR_PRODUCT_K; };
+        // the tile that is being loaded
+        ProductWork ahead;
+        uint32_t loading = 0;
+        bool more = true;
+        const uint16_t *pn, *qn;
         uint32_t po[P_KINDS], qo[Q_KINDS];
-#pragma unroll
-        for (int i = 0; i < P_KINDS; ++i) po[i] = source<P_OUTER, BM, true>((wave + i * WAVES) % P_ROWS, lane, P.ld, P.extent - p0, IVFR_PRODUCT_K);
-#pragma unroll
-        for (int i = 0; i < Q_KINDS; ++i) qo[i] = source<Q_OUTER, BN, false>((wave + i * WAVES) % Q_ROWS, lane, Q.ld, Q.extent - q0, IVFR_PRODUCT_K);
-        const int stages = (count + KSUB - 1) / KSUB;
         int at = 0;   // first slice of the next stage to load
-        // The next stage goes to buffer `buf`.  Past the last slice that one again, so that the number of loads in flight is always the same.
+        auto begin = [&]() {
+            const int p0 = ahead.p * BM, q0 = ahead.q * BN;
+            pn = P.base + ahead.p_at + (P_OUTER ? (p0 >> 8) * P.panel + (p0 & 255) : p0 * P.ld);
+            qn = Q.base + ahead.q_at + (Q_OUTER ? (q0 >> 8) * Q.panel + (q0 & 255) : q0 * Q.ld);
+            at = 0;
+#pragma unroll
+            for (int i = 0; i < P_KINDS; ++i) po[i] = source<P_OUTER, BM, true>((wave + i * WAVES) % P_ROWS, lane, P.ld, P.extent - p0, IVFR_PRODUCT_K);
+#pragma unroll
+            for (int i = 0; i < Q_KINDS; ++i) qo[i] = source<Q_OUTER, BN, false>((wave + i * WAVES) % Q_ROWS, lane, Q.ld, Q.extent - q0, IVFR_PRODUCT_K);
+        };
+        if (!work(loading, ahead)) return;   // uniform
+        begin();
+        // The next stage goes to buffer `buf`.  Past the last slice of all tiles that one again, so that the number of loads in flight is always the same.
         auto load = [&](int buf) {
+            if (at >= ahead.count && more) {   // uniform
+                more = work(++loading, ahead);
+                if (more) begin();
+            }
             const uint32_t base = lds0 + buf * STAGE;
 #pragma unroll
             for (int i = 0; i < P_EACH; ++i) {
                 const int f = (wave + i * WAVES) % P_LOADS, row = f % P_ROWS, plane = f / P_ROWS % PLANES, sub = f / (P_ROWS * PLANES);
-                const int slice = at + sub < count ? at + sub : count - 1;
+                const int slice = ahead.first + (at + sub < ahead.count ? at + sub : ahead.count - 1);
                 uint32_t o = po[i % P_KINDS];
-                if constexpr (P_OUTER) o = source<true, BM, true>(row, lane, P.ld, P.extent - p0, P.rows - (first + slice) * IVFR_PRODUCT_K);
-                load16(base + sub * SLICE + plane * P_SLICE + 1024 * row, o, pn + slice * pstep + (PLANES > 1 ? plane * P.plane : 0));
+                if constexpr (P_OUTER) {
+                    const int left = P.rows - slice * IVFR_PRODUCT_K;
+                    if (left < IVFR_PRODUCT_K) o = source<true, BM, true>(row, lane, P.ld, P.extent - ahead.p * BM, left);   // uniform
+                }
+                load16(base + sub * SLICE + plane * P_SLICE + 1024 * row, o, pn + slice_at(P, P_OUTER, slice) + (PLANES > 1 ? plane * P.plane : 0));
             }
 #pragma unroll
             for (int i = 0; i < Q_EACH; ++i) {
                 const int f = (wave + i * WAVES) % Q_LOADS, row = f % Q_ROWS, plane = f / Q_ROWS % PLANES, sub = f / (Q_ROWS * PLANES);
-                const int slice = at + sub < count ? at + sub : count - 1;
+                const int slice = ahead.first + (at + sub < ahead.count ? at + sub : ahead.count - 1);
                 uint32_t o = qo[i % Q_KINDS];
-                if constexpr (Q_OUTER) o = source<true, BN, false>(row, lane, Q.ld, Q.extent - q0, Q.rows - (first + slice) * IVFR_PRODUCT_K);
-                load16(base + sub * SLICE + PLANES * P_SLICE + plane * Q_SLICE + 1024 * row, o, qn + slice * qstep + (PLANES > 1 ? plane * Q.plane : 0));
+                if constexpr (Q_OUTER) {
+                    const int left = Q.rows - slice * IVFR_PRODUCT_K;
+                    if (left < IVFR_PRODUCT_K) o = source<true, BN, false>(row, lane, Q.ld, Q.extent - ahead.q * BN, left);
+                }
+                load16(base + sub * SLICE + PLANES * P_SLICE + plane * Q_SLICE + 1024 * row, o, qn + slice_at(Q, Q_OUTER, slice) + (PLANES > 1 ? plane * Q.plane : 0));
             }
             at += KSUB;
         };
@@ -186,11 +216,8 @@ struct Product {
             if constexpr (Q_OUTER) return outer_read(b, qf, wn + 16 * t, qk);
             else return *reinterpret_cast<const short8v*>(b + qf[0] + t * 16 * KB);
         };
-#pragma unroll
-        for (int a = 0; a < TM; ++a)
-#pragma unroll
-            for (int b = 0; b < TN; ++b) acc[a][b] = floatx4{0.f, 0.f, 0.f, 0.f};
-        if (count <= 0) return;   // uniform
+        floatx4 acc[TM][TN];
+        ProductWork w;
 #pragma unroll
         for (int s = 0; s < STAGES - 1; ++s) load(s);
         int buf = 0;   // of the stage that is being used
@@ -205,10 +232,10 @@ struct Product {
             for (int t = 0; t < TN; ++t) fq[0][t] = read_q(smem, 0, t);
 #pragma unroll
             for (int t = 0; t < TM; ++t) fp[t] = read_p(smem, 0, t);
-            // slice number `sub` of its stage
-            auto step = [&](int sub, short8v (&cq)[TN], short8v (&nq)[TN]) {
+            // slice number `sub` of its stage; `last` of its tile
+            auto step = [&](int sub, bool last, short8v (&cq)[TN], short8v (&nq)[TN]) {
                 const char* from = smem + buf * STAGE + (sub + 1) * SLICE;
-                if (sub + 1 == KSUB) {
+                if (sub + 1 == KSUB || last) {
                     wait_and_meet<(STAGES - 3) * EACH, (READS < 15 ? READS : 15)>();
                     load(buf == 0 ? STAGES - 1 : buf - 1);
                     buf = buf + 1 == STAGES ? 0 : buf + 1;
@@ -231,55 +258,82 @@ struct Product {
                 }
                 __builtin_amdgcn_sched_barrier(0);
             };
-            // (after the last slice the reads bring what nothing uses: the stages past the end hold the last slice again)
             constexpr int UNROLL = KSUB == 1 ? 2 : KSUB;
-            for (int done = 0;;) {
+            for (uint32_t tile = 0; work(tile, w); ++tile) {
 #pragma unroll
-                for (int i = 0; i < UNROLL; ++i) {
-                    step(i % KSUB, fq[i & 1], fq[(i + 1) & 1]);
-                    if (++done == count) break;
+                for (int a = 0; a < TM; ++a)
+#pragma unroll
+                    for (int b = 0; b < TN; ++b) acc[a][b] = floatx4{0.f, 0.f, 0.f, 0.f};
+                bool odd = false;   // the next fragments of Q are in fq[1]
+                for (int left = w.count;;) {
+#pragma unroll
+                    for (int i = 0; i < UNROLL; ++i) {
+                        step(i % KSUB, left == 1, fq[i & 1], fq[(i + 1) & 1]);
+                        odd = (i + 1) & 1;
+                        if (--left == 0) break;
+                    }
+                    if (left == 0) break;
                 }
-                if (done == count) break;
+                if (odd) {   // uniform
+#pragma unroll
+                    for (int b = 0; b < TN; ++b) fq[0][b] = fq[1][b];
+                }
+                done(w, acc);
             }
         } else {
-            for (int s = 0; s < stages; ++s) {
-                // loaded are the stages up to s + STAGES - 2
-                wait_and_meet<(STAGES - 2) * EACH, 0>();
-                load(buf == 0 ? STAGES - 1 : buf - 1);   // (all have read stage s - 1)
+            for (uint32_t tile = 0; work(tile, w); ++tile) {
 #pragma unroll
-                for (int sub = 0; sub < KSUB; ++sub) {
-                    if (KSUB > 1 && s * KSUB + sub >= count) break;   // uniform
-                    const char* const from = smem + buf * STAGE + sub * SLICE;
-                    short8v fp[PLANES][TM], fq[PLANES][TN];
+                for (int a = 0; a < TM; ++a)
 #pragma unroll
-                    for (int n = PLANES - 1; n >= 0; --n) {
+                    for (int b = 0; b < TN; ++b) acc[a][b] = floatx4{0.f, 0.f, 0.f, 0.f};
+                for (int s = 0; s < w.count; s += KSUB) {
+                    // loaded are the stages up to the one after the next STAGES - 2
+                    wait_and_meet<(STAGES - 2) * EACH, 0>();
+                    load(buf == 0 ? STAGES - 1 : buf - 1);   // (all have read the stage before)
 #pragma unroll
-                        for (int t = 0; t < TN; ++t) fq[n][t] = read_q(from, n, t);
+                    for (int sub = 0; sub < KSUB; ++sub) {
+                        if (KSUB > 1 && s + sub >= w.count) break;   // uniform
+                        const char* const from = smem + buf * STAGE + sub * SLICE;
+                        short8v fp[PLANES][TM], fq[PLANES][TN];
 #pragma unroll
-                        for (int t = 0; t < TM; ++t) fp[n][t] = read_p(from, n, t);
+                        for (int n = PLANES - 1; n >= 0; --n) {
+#pragma unroll
+                            for (int t = 0; t < TN; ++t) fq[n][t] = read_q(from, n, t);
+#pragma unroll
+                            for (int t = 0; t < TM; ++t) fp[n][t] = read_p(from, n, t);
+                        }
+#pragma unroll
+                        for (int sum = PLANES - 1; sum >= 0; --sum)   // small products first
+#pragma unroll
+                            for (int n = 0; n <= sum; ++n)
+#pragma unroll
+                                for (int a = 0; a < TM; ++a)
+#pragma unroll
+                                    for (int b = 0; b < TN; ++b) acc[a][b] = mfma(fp[n][a], fq[sum - n][b], acc[a][b]);
                     }
-#pragma unroll
-                    for (int sum = PLANES - 1; sum >= 0; --sum)   // small products first
-#pragma unroll
-                        for (int n = 0; n <= sum; ++n)
-#pragma unroll
-                            for (int a = 0; a < TM; ++a)
-#pragma unroll
-                                for (int b = 0; b < TN; ++b) acc[a][b] = mfma(fp[n][a], fq[sum - n][b], acc[a][b]);
+                    buf = buf + 1 == STAGES ? 0 : buf + 1;
                 }
-                buf = buf + 1 == STAGES ? 0 : buf + 1;
+                done(w, acc);
             }
         }
-        wait_and_meet<0, 0>();   // nothing is on its way to LDS, which may be used for something else from here on
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing of this wavefront is on its way to LDS when its workgroup gives that up
     }
+    // between wavefronts, without waiting for what is on its way to the stages
+    static __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-    // first p (of four, or with P inner of eight in the tiles t, t + 1) and q of this lane's outputs in tile (t, u)
-    static __device__ __forceinline__ int p_of(int t) {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / WAVES_N * (BM / WAVES_M);
+    // This thread, for what is done with a tile: not known to be the same for every tile, so that nothing formed of it is kept in registers over the products.
+    static __device__ __forceinline__ int thread() {
+        int t = threadIdx.x;
+        asm volatile("" : "+v"(t));
+        return t;
+    }
+    // first p (of four, or with P inner of eight in the tiles t, t + 1) and q of a thread's outputs in tile (t, u)
+    static __device__ __forceinline__ int p_of(int thread, int t) {
+        const int lane = thread & 63, wave = thread >> 6, wm = wave / WAVES_N * (BM / WAVES_M);
         return P_OUTER ? wm + 16 * t + 4 * (lane >> 4) : wm + 16 * (t & ~1) + 8 * (lane >> 4) + 4 * (t & 1);
     }
-    static __device__ __forceinline__ int q_of(int u) {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    static __device__ __forceinline__ int q_of(int thread, int u) {
+        const int lane = thread & 63, wave = thread >> 6;
         return wave % WAVES_N * (BN / WAVES_N) + 16 * u + (lane & 15);
     }
 };

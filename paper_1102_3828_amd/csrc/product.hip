@@ -26,41 +26,47 @@ __device__ __forceinline__ void store_four(void* out, int64_t at, int type, cons
 }
 
 template <class C>
-__device__ __forceinline__ void form(const ProductOut& o, uint32_t block, char* smem) {
-    const ProductTile tile = product_tile(block, (o.np + C::BM - 1) / C::BM, (o.nq + C::BN - 1) / C::BN, o.splits);
-    if (!tile.any) return;   // uniform
-    const int per = (o.slices + o.splits - 1) / o.splits;
-    const int p0 = tile.p * C::BM, q0 = tile.q * C::BN, first = tile.split * per;
-    floatx4 acc[C::TM][C::TN];
-    C::run(o.P, o.Q, p0, q0, first, o.slices - first < per ? o.slices - first : per, smem, acc);
+__device__ __forceinline__ void form(const ProductOut& o, uint32_t block, uint32_t blocks, char* smem) {
+    const int tiles_p = (o.np + C::BM - 1) / C::BM, tiles_q = (o.nq + C::BN - 1) / C::BN, per = (o.slices + o.splits - 1) / o.splits;
     const float alpha = o.partial ? 1.f : o.alpha * (o.unit ? o.unit[1] : 1.f);
     const int64_t ld = o.partial ? (o.np + 3) / 4 * 4 : o.ld;
     const int type = o.partial ? IVFR_TYPE_F32 : o.type, limit = o.partial ? (int)ld : o.np;
-    void* const out = o.partial ? (void*)(o.partial + (int64_t)(o.slot0 + tile.split) * o.nq * ld) : o.out;
-    const bool whole = ld % 4 == 0 && ((uintptr_t)out & 15) == 0;   // uniform
+    C::run(o.P, o.Q, smem,
+           [&](uint32_t i, ProductWork& w) {
+               if (!product_work(i, block, blocks, tiles_p, tiles_q, o.splits, w)) return false;
+               w.first = w.split * per;
+               w.count = o.slices - w.first < per ? o.slices - w.first : per;
+               w.p_at = w.q_at = 0;
+               return true;
+           },
+           [&](const ProductWork& w, floatx4 (&acc)[C::TM][C::TN]) {
+               const int tid = C::thread(), p0 = w.p * C::BM, q0 = w.q * C::BN;
+               void* const out = o.partial ? (void*)(o.partial + (int64_t)(o.slot0 + w.split) * o.nq * ld) : o.out;
+               const bool whole = ld % 4 == 0 && ((uintptr_t)out & 15) == 0;   // uniform
 #pragma unroll
-    for (int u = 0; u < C::TN; ++u) {
-        const int q = q0 + C::q_of(u);
-        if (q >= o.nq) continue;
+               for (int u = 0; u < C::TN; ++u) {
+                   const int q = q0 + C::q_of(tid, u);
+                   if (q >= o.nq) continue;
 #pragma unroll
-        for (int t = 0; t < C::TM; ++t) {
-            const int p = p0 + C::p_of(t);
-            if (p < limit) store_four(out, q * ld + p, type, acc[t][u] * alpha, limit - p, whole);
-        }
-    }
+                   for (int t = 0; t < C::TM; ++t) {
+                       const int p = p0 + C::p_of(tid, t);
+                       if (p < limit) store_four(out, q * ld + p, type, acc[t][u] * alpha, limit - p, whole);
+                   }
+               }
+           });
 }
 
 template <class C>
 __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void out_kernel(ProductOut o) {
     __shared__ __align__(1024) char smem[C::LDS];
-    form<C>(o, blockIdx.x, smem);
+    form<C>(o, blockIdx.x, gridDim.x, smem);
 }
 // The first `blocks` workgroups form x, the others w.
 template <class CX, class CW>
 __global__ __launch_bounds__(CX::THREADS, CX::WAVES_SIMD) void two_out_kernel(ProductOut x, ProductOut w, uint32_t blocks) {
     __shared__ __align__(1024) char smem[CX::LDS > CW::LDS ? CX::LDS : CW::LDS];
-    if (blockIdx.x < blocks) form<CX>(x, blockIdx.x, smem);
-    else form<CW>(w, blockIdx.x - blocks, smem);
+    if (blockIdx.x < blocks) form<CX>(x, blockIdx.x, blocks, smem);
+    else form<CW>(w, blockIdx.x - blocks, gridDim.x - blocks, smem);
 }
 
 // A thread takes four neighbouring values through all slots.
@@ -123,14 +129,15 @@ void product_cut(int64_t np, int64_t nq, int64_t slices, int planes, bool q_oute
     }
 }
 
+template <class C>
 static unsigned out_blocks(const ProductOut& o) {
-    return product_grid((int64_t)((o.np + IVFR_TILE_P[o.tile] - 1) / IVFR_TILE_P[o.tile]) * ((o.nq + IVFR_TILE_Q[o.tile] - 1) / IVFR_TILE_Q[o.tile]) * o.splits);
+    return product_grid((int64_t)((o.np + C::BM - 1) / C::BM) * ((o.nq + C::BN - 1) / C::BN) * o.splits, C::RESIDENT);
 }
 
 template <int TILE, bool QO, bool HALF, int PLANES>
 static int launch_one(const ProductOut& o, hipStream_t st) {
     typedef typename ProductOf<TILE, true, QO, HALF, PLANES>::T C;
-    hipLaunchKernelGGL((out_kernel<C>), dim3(out_blocks(o)), dim3(C::THREADS), 0, st, o);
+    hipLaunchKernelGGL((out_kernel<C>), dim3(out_blocks<C>(o)), dim3(C::THREADS), 0, st, o);
     IVFR_HIP(hipGetLastError());
     return IVFR_OK;
 }
@@ -153,8 +160,8 @@ template <int TILE, bool HALF, int PLANES>
 static int launch_two(const ProductOut& x, const ProductOut& w, hipStream_t st) {
     typedef typename ProductOf<TILE, true, false, HALF, PLANES>::T CX;
     typedef typename ProductOf<TILE, true, true, HALF, PLANES>::T CW;
-    const unsigned blocks = out_blocks(x);
-    hipLaunchKernelGGL((two_out_kernel<CX, CW>), dim3(blocks + out_blocks(w)), dim3(CX::THREADS), 0, st, x, w, blocks);
+    const unsigned blocks = out_blocks<CX>(x);
+    hipLaunchKernelGGL((two_out_kernel<CX, CW>), dim3(blocks + out_blocks<CW>(w)), dim3(CX::THREADS), 0, st, x, w, blocks);
     IVFR_HIP(hipGetLastError());
     return IVFR_OK;
 }

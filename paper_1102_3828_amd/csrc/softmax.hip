@@ -16,11 +16,11 @@
 
 // ---------------------------------------------------------------- operands
 
-// rows of src in 16-bit planes, padded with zeros to rows_out x ld_out; rows that take no part are zero, whatever they hold:
+// rows of src in 16-bit planes, padded with zeros to rows_out x columns_out; rows that take no part are zero, whatever they hold:
 // left out by an infinite negative offset, or without a target
 struct PackArgs {
     const void* src;
-    int64_t ld, rows, rows_out, ld_out;
+    int64_t ld, rows, rows_out, columns_out, ld_out;
     int d, vec;                // vec: rows start at 16-byte boundaries
     uint16_t* dst;
     const float* offset;       // [rows] or null
@@ -38,7 +38,7 @@ struct UnitArgs {
 
 template <bool F32>
 __device__ __forceinline__ void pack(const PackArgs& a, int64_t block) {
-    const int64_t chunks = a.ld_out / 8, total = a.rows_out * chunks;
+    const int64_t chunks = a.columns_out / 8, total = a.rows_out * chunks;
     for (int64_t i = block * 256 + threadIdx.x; i < total; i += (int64_t)a.blocks * 256) {
         const int64_t row = i / chunks;
         const int k0 = (int)(i - row * chunks) * 8;
@@ -127,61 +127,61 @@ struct ScoreArgs {
     const float* lse;          // [n]
     const float* weight;       // [n]
     const float* unit;         // unit[0] is a factor of e, or null
-    uint16_t* e;               // [planes][n_pad][e_ld]
-    int64_t e_ld;
+    uint16_t* e;               // [planes][panels of 256 vectors][n_pad][256]
+    int64_t e_plane;           // elements of a plane
     int n_pad, v_pad;          // rows and columns of e that are written (zeros beyond n and v)
 };
 
 #define LOG2E 1.44269504088896340736f
 #define LN2 0.69314718055994530942f
 
-// scores of this lane's outputs times log2 e (exponentials are powers of two from here on), in place; vectors that take no part, or do not exist: -inf
-template <class C>
-__device__ __forceinline__ void scores(float scale, const float* offset, int v, int p0, floatx4 (&acc)[C::TM][C::TN]) {
-    if (!offset && p0 + C::BM <= v) {   // uniform
-#pragma unroll
-        for (int t = 0; t < C::TM; ++t)
-#pragma unroll
-            for (int u = 0; u < C::TN; ++u) acc[t][u] *= scale;
-        return;
-    }
+// Scores of this lane's outputs times log2 e (exponentials are powers of two from here on), in place; vectors that take no part, or do not exist: -inf.
+// SOME: there may be such vectors, or offsets.
+template <class C, bool SOME>
+__device__ __forceinline__ void scores(float scale, const float* offset, int v, int tid, int p0, floatx4 (&acc)[C::TM][C::TN]) {
 #pragma unroll
     for (int t = 0; t < C::TM; ++t) {
-        const int j = p0 + C::p_of(t);
-        float o[4];
+        float o[4] = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (SOME) {
+            const int j = p0 + C::p_of(tid, t);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) o[r] = j + r < v ? (offset ? offset[j + r] * LOG2E : 0.f) : -INFINITY;
+            for (int r = 0; r < 4; ++r) o[r] = j + r < v ? (offset ? offset[j + r] * LOG2E : 0.f) : -INFINITY;
+        }
 #pragma unroll
         for (int u = 0; u < C::TN; ++u)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) acc[t][u][r] = o[r] == -INFINITY ? -INFINITY : fmaf(acc[t][u][r], scale, o[r]);
+            for (int r = 0; r < 4; ++r) {
+                if constexpr (SOME) acc[t][u][r] = o[r] == -INFINITY ? -INFINITY : fmaf(acc[t][u][r], scale, o[r]);
+                else acc[t][u][r] *= scale;
+            }
     }
 }
 
 // Which of this lane's outputs (4 t + r) of a column is at row `at` of the tile; negative if none is.
 template <class C>
-__device__ __forceinline__ int output_at(int at) {
-    const int lane = threadIdx.x & 63, rel = at - (int)(threadIdx.x >> 6) / C::WAVES_N * (C::BM / C::WAVES_M);
+__device__ __forceinline__ int output_at(int tid, int at) {
+    const int lane = tid & 63, rel = at - (tid >> 6) / C::WAVES_N * (C::BM / C::WAVES_M);
     return at < 0 || rel < 0 || rel >= C::BM / C::WAVES_M || ((rel >> 3) & 3) != lane >> 4 ? -1 : (rel >> 5) * 8 + (rel & 7);
 }
 
-template <class C>
-__global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void score_kernel(ScoreArgs a) {
-    __shared__ __align__(1024) char smem[C::LDS];
-    const ProductTile tile = product_tile(blockIdx.x, a.tiles_p, a.tiles_q, 1);
-    if (!tile.any) return;   // uniform
-    const int p0 = tile.p * C::BM, q0 = tile.q * C::BN;
-    floatx4 acc[C::TM][C::TN];
-    C::run(a.w, a.x, p0, q0, 0, a.slices, smem, acc);
-    scores<C>(a.scale, a.offset, a.v, p0, acc);
-    __syncthreads();   // the stages are no longer read
-    float2* const red = reinterpret_cast<float2*>(smem);   // [WAVES_M][BN]
-    const int lane = threadIdx.x & 63, wm = (threadIdx.x >> 6) / C::WAVES_N;
+__device__ __forceinline__ bool score_work(const ScoreArgs& a, uint32_t i, ProductWork& w) {
+    w.first = 0;
+    w.count = a.slices;
+    w.p_at = w.q_at = 0;
+    return product_work(i, blockIdx.x, gridDim.x, a.tiles_p, a.tiles_q, 1, w);
+}
+
+// a tile's statistics; red: [WAVES_M][BN]
+template <class C, bool SOME>
+__device__ __forceinline__ void reduce_scores(const ScoreArgs& a, const ProductWork& tile, floatx4 (&acc)[C::TM][C::TN], float2* red) {
+    const int tid = C::thread(), p0 = tile.p * C::BM, q0 = tile.q * C::BN;
+    scores<C, SOME>(a.scale, a.offset, a.v, tid, p0, acc);
+    const int lane = tid & 63, wm = (tid >> 6) / C::WAVES_N;
 #pragma unroll
     for (int u = 0; u < C::TN; ++u) {
-        const int i = q0 + C::q_of(u);
+        const int i = q0 + C::q_of(tid, u);
         const int64_t target = i < a.n ? a.targets[i] : -1;
-        const int own = output_at<C>(target >= p0 && target < a.v && target < p0 + C::BM ? (int)target - p0 : -1);
+        const int own = output_at<C>(tid, target >= p0 && target < a.v && target < p0 + C::BM ? (int)target - p0 : -1);
         if (own >= 0) {   // one lane of the launch
             float z = 0.f;
 #pragma unroll
@@ -208,10 +208,10 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void score_kernel(ScoreA
             for (int r = 0; r < 4; ++r) s += __builtin_amdgcn_exp2f(acc[t][u][r] - base);
         s += __shfl_xor(s, 16, 64);
         s += __shfl_xor(s, 32, 64);
-        if (lane < 16) red[wm * C::BN + C::q_of(u)] = make_float2(m, s);
+        if (lane < 16) red[wm * C::BN + C::q_of(tid, u)] = make_float2(m, s);
     }
-    __syncthreads();
-    for (int q = threadIdx.x; q < C::BN; q += C::THREADS) {
+    C::meet();
+    for (int q = tid; q < C::BN; q += C::THREADS) {
         const int i = q0 + q;
         if (i >= a.n) continue;
         float m = -INFINITY;
@@ -223,6 +223,17 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void score_kernel(ScoreA
         for (int w = 0; w < C::WAVES_M; ++w) s += red[w * C::BN + q].y * __builtin_amdgcn_exp2f(red[w * C::BN + q].x - base);
         a.part[(int64_t)i * a.tiles_p + tile.p] = make_float2(m, s);
     }
+}
+
+template <class C>
+__global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void score_kernel(ScoreArgs a) {
+    __shared__ __align__(1024) char smem[C::LDS];
+    __shared__ float2 red[C::WAVES_M * C::BN];
+    C::run(a.w, a.x, smem, [&](uint32_t i, ProductWork& w) { return score_work(a, i, w); },
+           [&](const ProductWork& tile, floatx4 (&acc)[C::TM][C::TN]) {
+               if (a.offset || (tile.p + 1) * C::BM > a.v) reduce_scores<C, true>(a, tile, acc, red);   // uniform
+               else reduce_scores<C, false>(a, tile, acc, red);
+           });
 }
 
 // A wavefront per row joins its tiles' statistics (in a fixed order).
@@ -264,19 +275,13 @@ __global__ __launch_bounds__(256) void loss_kernel(const float2* __restrict__ pa
 
 // ---------------------------------------------------------------- gradient
 
-template <class C>
-__global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void grad_score_kernel(ScoreArgs a) {
-    __shared__ __align__(1024) char smem[C::LDS];
-    const ProductTile tile = product_tile(blockIdx.x, a.tiles_p, a.tiles_q, 1);
-    if (!tile.any) return;   // uniform
-    const int p0 = tile.p * C::BM, q0 = tile.q * C::BN;
-    floatx4 acc[C::TM][C::TN];
-    C::run(a.w, a.x, p0, q0, 0, a.slices, smem, acc);
-    scores<C>(a.scale, a.offset, a.v, p0, acc);
-    const float unit = a.unit ? a.unit[0] : 1.f;
+template <class C, bool SOME>
+__device__ __forceinline__ void write_factors(const ScoreArgs& a, const ProductWork& tile, floatx4 (&acc)[C::TM][C::TN], float unit) {
+    const int tid = C::thread(), p0 = tile.p * C::BM, q0 = tile.q * C::BN;
+    scores<C, SOME>(a.scale, a.offset, a.v, tid, p0, acc);
 #pragma unroll
     for (int u = 0; u < C::TN; ++u) {
-        const int i = q0 + C::q_of(u);
+        const int i = q0 + C::q_of(tid, u);
         if (i >= a.n_pad) continue;
         int64_t target = -1;
         float L = 0.f, g = 0.f;
@@ -294,7 +299,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void grad_score_kernel(S
         {   // the row's own vector, if it is in this tile and takes part: p - 1 before anything is rounded
             int at = target >= (int64_t)a.v0 + p0 && target < (int64_t)a.v0 + a.v && target < (int64_t)a.v0 + p0 + C::BM ? (int)(target - a.v0 - p0) : -1;
             if (at >= 0 && a.offset && a.offset[p0 + at] == -INFINITY) at = -1;
-            const int own = output_at<C>(at);
+            const int own = output_at<C>(tid, at);
             if (own >= 0) {
 #pragma unroll
                 for (int t = 0; t < C::TM; ++t)
@@ -305,12 +310,12 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void grad_score_kernel(S
         const bool live = g != 0.f;   // (a row without gradient: zeros, whatever its statistics are)
 #pragma unroll
         for (int t = 0; t < C::TM; t += 2) {
-            const int j = p0 + C::p_of(t);
+            const int j = p0 + C::p_of(tid, t);
             if (j >= a.v_pad) continue;   // (a multiple of 8, as j)
             float f[8];
 #pragma unroll
             for (int r = 0; r < 8; ++r) f[r] = g * acc[t + (r >> 2)][u][r & 3];
-            uint16_t* const o = a.e + (int64_t)i * a.e_ld + j;
+            uint16_t* const o = a.e + ((int64_t)(j >> 8) * a.n_pad + i) * 256 + (j & 255);
 #pragma unroll
             for (int p = 0; p < C::PLANES; ++p) {
                 short8v h;
@@ -324,10 +329,20 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void grad_score_kernel(S
                     }
                 }
                 if (!live) h = short8v{0, 0, 0, 0, 0, 0, 0, 0};
-                *reinterpret_cast<short8v*>(o + (int64_t)p * a.n_pad * a.e_ld) = h;
+                *reinterpret_cast<short8v*>(o + p * a.e_plane) = h;
             }
         }
-    }
+    }}
+
+template <class C>
+__global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void grad_score_kernel(ScoreArgs a) {
+    __shared__ __align__(1024) char smem[C::LDS];
+    const float unit = a.unit ? a.unit[0] : 1.f;
+    C::run(a.w, a.x, smem, [&](uint32_t i, ProductWork& w) { return score_work(a, i, w); },
+           [&](const ProductWork& tile, floatx4 (&acc)[C::TM][C::TN]) {
+               if (a.offset || (tile.p + 1) * C::BM > a.v) write_factors<C, true>(a, tile, acc, unit);   // uniform
+               else write_factors<C, false>(a, tile, acc, unit);
+           });
 }
 
 // ---------------------------------------------------------------- host
@@ -343,7 +358,7 @@ static int score_tile(int64_t n, int64_t v, int planes) {
 template <int TILE, bool HALF, int PLANES>
 static int launch_score_tile(const ScoreArgs& a, bool grad, hipStream_t st) {
     typedef typename ProductOf<TILE, false, false, HALF, PLANES>::T C;
-    const dim3 grid(product_grid((int64_t)a.tiles_p * a.tiles_q));
+    const dim3 grid(product_grid((int64_t)a.tiles_p * a.tiles_q, C::RESIDENT));
     if (grad) hipLaunchKernelGGL((grad_score_kernel<C>), grid, dim3(C::THREADS), 0, st, a);
     else hipLaunchKernelGGL((score_kernel<C>), grid, dim3(C::THREADS), 0, st, a);
     IVFR_HIP(hipGetLastError());
@@ -376,7 +391,7 @@ static inline int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * 
 struct SoftmaxPlan {
     int planes, slices, tile;
     bool half, pack_x, pack_w;
-    int64_t kd, n_pad, e_ld, piece;   // columns of packed operands; rows and columns of e, vectors a piece
+    int64_t kd, ld, n_pad, e_plane, piece;   // columns of packed operands, elements between their rows; rows of e, elements of its planes, vectors a piece
     int pieces;
     int64_t tiles_p;                  // of the loss
     int dx_tile, dx_splits, dw_tile, dw_splits;   // of a whole piece
@@ -404,6 +419,7 @@ static SoftmaxPlan softmax_plan(const ivfr_softmax_args& a, bool grad) {
     p.planes = f32 ? 3 : 1;
     p.kd = round_up(a.d, 32);
     p.slices = (int)(p.kd / 32);
+    p.ld = product_ld(p.kd);
     p.n_pad = round_up(a.n, 32);
     // gradients read x by rows of k: padded to whole stages; rows that take no part are zeroed in the copy
     p.pack_x = f32 || grad || a.d % 32 || !rows_aligned(a.x, a.ldx, 2);
@@ -414,8 +430,8 @@ static SoftmaxPlan softmax_plan(const ivfr_softmax_args& a, bool grad) {
         at += round_up(bytes, 256);
         return here;
     };
-    if (p.pack_x) p.at_x = take(p.planes * (grad ? p.n_pad : a.n) * p.kd * 2);
-    if (p.pack_w) p.at_w = take(p.planes * a.v * p.kd * 2);
+    if (p.pack_x) p.at_x = take(p.planes * (grad ? p.n_pad : a.n) * p.ld * 2);
+    if (p.pack_w) p.at_w = take(p.planes * a.v * p.ld * 2);
     p.tile = score_tile(a.n, a.v, p.planes);
     p.tiles_p = (a.v + IVFR_TILE_P[p.tile] - 1) / IVFR_TILE_P[p.tile];
     p.at_part = take(a.n * p.tiles_p * 8);
@@ -428,8 +444,8 @@ static SoftmaxPlan softmax_plan(const ivfr_softmax_args& a, bool grad) {
         p.pieces = (int)((a.v + fit - 1) / fit);
         p.piece = std::min(round_up((a.v + p.pieces - 1) / p.pieces, 256), round_up(a.v, 32));
         p.pieces = (int)((a.v + p.piece - 1) / p.piece);
-        p.e_ld = round_up(p.piece, 64) + 64;   // (not a large power of two: rows would all begin in the same memory channel)
-        p.at_e = take(p.planes * p.n_pad * p.e_ld * 2);
+        p.e_plane = (p.piece + 255) / 256 * p.n_pad * 256;
+        p.at_e = take(p.planes * p.e_plane * 2);
         product_cut(a.d, a.n, (p.piece + 31) / 32, p.planes, false, &p.dx_tile, &p.dx_splits);
         product_cut(a.d, p.piece, p.n_pad / 32, p.planes, true, &p.dw_tile, &p.dw_splits);
         if (p.pieces > 1 || p.dx_splits > 1) p.at_dx = take((int64_t)p.pieces * p.dx_splits * a.n * product_pad(a.d) * 4);
@@ -464,16 +480,16 @@ static int prepare(const ivfr_softmax_args& a, const SoftmaxPlan& p, const float
     s.w = {(const uint16_t*)a.w, 0, a.ldw, (int)a.v, 0};
     PackArgs x = {}, w = {};
     UnitArgs u = {};
-    auto blocks = [](const PackArgs& k) { return (unsigned)std::min<int64_t>((k.rows_out * (k.ld_out / 8) + 255) / 256, 4096); };
+    auto blocks = [](const PackArgs& k) { return (unsigned)std::min<int64_t>((k.rows_out * (k.columns_out / 8) + 255) / 256, 4096); };
     if (p.pack_x) {
-        x = {a.x, a.ldx, a.n, weight ? p.n_pad : a.n, p.kd, a.d, rows_aligned(a.x, a.ldx, f32 ? 4 : 2), (uint16_t*)(ws + p.at_x), nullptr, weight ? a.targets : nullptr, 0};
+        x = {a.x, a.ldx, a.n, weight ? p.n_pad : a.n, p.kd, p.ld, a.d, rows_aligned(a.x, a.ldx, f32 ? 4 : 2), (uint16_t*)(ws + p.at_x), nullptr, weight ? a.targets : nullptr, 0};
         x.blocks = blocks(x);
-        s.x = {x.dst, x.rows_out * p.kd, p.kd, (int)x.rows_out, 0};   // (the rows of e reach up to the padding)
+        s.x = {x.dst, x.rows_out * p.ld, p.ld, (int)x.rows_out, 0};   // (the rows of e reach up to the padding)
     }
     if (p.pack_w) {
-        w = {a.w, a.ldw, a.v, a.v, p.kd, a.d, rows_aligned(a.w, a.ldw, f32 ? 4 : 2), (uint16_t*)(ws + p.at_w), a.offset, nullptr, 0};
+        w = {a.w, a.ldw, a.v, a.v, p.kd, p.ld, a.d, rows_aligned(a.w, a.ldw, f32 ? 4 : 2), (uint16_t*)(ws + p.at_w), a.offset, nullptr, 0};
         w.blocks = blocks(w);
-        s.w = {w.dst, a.v * p.kd, p.kd, (int)a.v, 0};
+        s.w = {w.dst, a.v * p.ld, p.ld, (int)a.v, 0};
     }
     if (weight && p.half) {
         u = {weight, a.targets, (int)a.n, (float*)(ws + p.at_unit)};
@@ -551,11 +567,14 @@ int ivfr_softmax_loss_grad(const ivfr_softmax_args* args, const float* weight, c
     }
     s.lse = lse;
     s.e = (uint16_t*)(ws + p.at_e);
-    s.e_ld = p.e_ld;
+    s.e_plane = p.e_plane;
     s.n_pad = (int)p.n_pad;
     const bool parts = p.pieces > 1 || p.dx_splits > 1;
     const ProductOperand w = s.w;
     ProductOut ox = {}, ow = {};
+    int slots = 0;
+    // (the last piece may have too few slices for as many parts)
+    auto parts_of = [](int slices, int splits) { const int per = (slices + splits - 1) / splits; return (slices + per - 1) / per; };
     for (int i = 0; i < p.pieces; ++i) {
         const int64_t v0 = (int64_t)i * p.piece, here = std::min(p.piece, a.v - v0);
         s.v0 = (int)v0;
@@ -577,28 +596,29 @@ int ivfr_softmax_loss_grad(const ivfr_softmax_args* args, const float* weight, c
         ox.P = s.w;
         ox.P.extent = a.d;
         ox.P.rows = (int)here;
-        ox.Q = {s.e, p.n_pad * p.e_ld, p.e_ld, (int)a.n, 0};
+        ox.Q = {s.e, p.e_plane, 256, (int)a.n, 0, p.n_pad * 256};
         ox.slices = s.v_pad / 32;
         ox.nq = (int)a.n;
         ox.out = dx;
         ox.partial = parts ? (float*)(ws + p.at_dx) : nullptr;
-        ox.slot0 = i * p.dx_splits;
+        ox.slot0 = slots;
         ox.tile = p.dx_tile;
-        ox.splits = p.dx_splits;
+        ox.splits = parts_of(ox.slices, p.dx_splits);
+        slots += ox.splits;
         // dw [here, d]: over the rows
         ow.P = s.x;
         ow.P.extent = a.d;
         ow.P.rows = (int)p.n_pad;
-        ow.Q = {s.e, p.n_pad * p.e_ld, p.e_ld, (int)here, (int)p.n_pad};
+        ow.Q = {s.e, p.e_plane, 256, (int)here, (int)p.n_pad, p.n_pad * 256};
         ow.slices = (int)(p.n_pad / 32);
         ow.nq = (int)here;
         ow.out = (char*)dw + v0 * a.d * size;
         ow.partial = p.dw_splits > 1 ? (float*)(ws + p.at_dw) : nullptr;
         ow.slot0 = 0;
         ow.tile = p.dw_tile;
-        ow.splits = p.dw_splits;
+        ow.splits = parts_of(ow.slices, p.dw_splits);
         IVFR_TRY(product_launch(ox, ow, p.half, st));
-        IVFR_TRY(product_join(ox, parts && i + 1 == p.pieces ? p.pieces * p.dx_splits : 0, ow, p.dw_splits > 1 ? p.dw_splits : 0, st));
+        IVFR_TRY(product_join(ox, parts && i + 1 == p.pieces ? slots : 0, ow, ow.partial ? ow.splits : 0, st));
     }
     return IVFR_OK;
 }
