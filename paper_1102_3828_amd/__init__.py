@@ -10,5 +10,7 @@ _BINDING_NAMES = ("Index", "IvfrError", "EXPORTED", "LIB_PATH", "lib", "memory_r
 def __getattr__(name):
     if name == "binding" or name in _BINDING_NAMES:
         binding = importlib.import_module(".binding", __name__)
-        return binding if name == "binding" else getattr(binding, name)
+        value = binding if name == "binding" else getattr(binding, name)
+        globals()[name] = value   # (later uses do not come here again)
+        return value
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

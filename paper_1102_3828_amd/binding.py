@@ -6,6 +6,7 @@ library is not built, importing this module raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -290,92 +291,83 @@ class Index:
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
-class _Call:
-    """The stream of a call, and the tensors it needs allocated for that stream (they may be freed while the call is still under way)."""
-
-    def __init__(self, device, stream):
-        self.device = device
-        self.stream = torch.cuda.current_stream(device) if stream is None else torch.cuda.ExternalStream(stream, device=device)
-
-    def __enter__(self):
-        self._guard = torch.cuda.stream(self.stream)
-        self._guard.__enter__()
-        return self
-
-    def __exit__(self, *exc):
-        return self._guard.__exit__(*exc)
-
-    @property
-    def handle(self):
-        return ctypes.c_void_p(self.stream.cuda_stream)
-
-    def empty(self, shape, dtype):
-        return torch.empty(shape, dtype=dtype, device=self.device)
+def _on(stream, device):
+    """(handle, context) of a call: its tensors are allocated for its stream, since they may be freed while the call is still under way."""
+    if stream is None:
+        return torch.cuda.current_stream(device).cuda_stream, contextlib.nullcontext()
+    return stream, torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device))
 
 
 def _rows(a, name):
-    """A matrix of a supported type whose rows are contiguous (they may lie further apart than their length)."""
-    if a.dim() != 2 or a.dtype not in _TYPES or not a.is_cuda:
+    """A matrix of a supported type whose rows are contiguous (they may lie further apart than their length), its type and leading dimension."""
+    kind = _TYPES.get(a.dtype)
+    if kind is None or a.dim() != 2 or not a.is_cuda:
         raise ValueError(f"{name} must be a float32, float16 or bfloat16 matrix on the GPU")
-    if a.shape[0] <= 1:
-        return a.contiguous(), max(a.shape[1], 1)
-    if a.shape[1] > 1 and a.stride(1) != 1 or a.stride(0) < a.shape[1]:
-        a = a.contiguous()
-    return a, a.stride(0)
+    n, d = a.shape
+    ld, inner = a.stride()
+    if n <= 1 or (d > 1 and inner != 1) or ld < d:
+        return a.contiguous(), kind, max(d, 1)
+    return a, kind, ld
 
 
 def _softmax_args(x, w, targets, scale, offset):
-    x, ldx = _rows(x, "x")
-    w, ldw = _rows(w, "w")
+    x, kind, ldx = _rows(x, "x")
+    w, w_kind, ldw = _rows(w, "w")
+    device = x.device
     n, d = x.shape
-    if w.shape[1] != d or w.dtype != x.dtype or w.device != x.device:
+    v = w.shape[0]
+    if w.shape[1] != d or w_kind != kind or w.device != device:
         raise ValueError("x and w must have the same number of components, type and device")
-    if targets.shape != (n,) or targets.dtype not in (torch.int64, torch.int32) or targets.device != x.device:
+    if targets.shape != (n,) or targets.dtype not in (torch.int64, torch.int32) or targets.device != device:
         raise ValueError("targets must be int64 or int32 [n] on the device of x")
     targets = targets.to(torch.int64).contiguous()
     if offset is not None:
-        if offset.shape != (w.shape[0],) or offset.dtype != torch.float32 or offset.device != x.device:
+        if offset.shape != (v,) or offset.dtype != torch.float32 or offset.device != device:
             raise ValueError("offset must be float32 [v] on the device of x")
         offset = offset.contiguous()
-    args = SoftmaxArgs(n, w.shape[0], d, _TYPES[x.dtype], x.data_ptr(), ldx, w.data_ptr(), ldw, targets.data_ptr(),
-                       None if offset is None else offset.data_ptr(), float(scale), x.device.index)
+    args = SoftmaxArgs(n, v, d, kind, x.data_ptr(), ldx, w.data_ptr(), ldw, targets.data_ptr(), None if offset is None else offset.data_ptr(),
+                       scale, device.index)
     return args, (x, w, targets, offset)   # (the tensors that the addresses belong to)
 
 
-def _softmax_workspace(args, grad, call):
+def _softmax_workspace(args, grad, device):
     need = ctypes.c_int64()
-    _check(lib.ivfr_softmax_workspace(ctypes.byref(args), int(grad), ctypes.byref(need)))
-    return call.empty(need.value, torch.uint8), need.value
+    _check(lib.ivfr_softmax_workspace(ctypes.byref(args), grad, ctypes.byref(need)))
+    return torch.empty(need.value, dtype=torch.uint8, device=device), need.value
 
 
 def softmax_loss(x, w, targets, scale=1.0, offset=None, stream=None):
     """Softmax cross entropy of the rows x [n, d] against the vectors w [v, d] (float32, float16 or bfloat16), without keeping the n x v
     scores scale * x w^T + offset.  targets: int64 or int32 [n], negative for rows without one.  offset: float32 [v] or None; -inf
     leaves a vector out.  Returns (loss, lse), float32 [n]; include/ivfadcr.h has the definitions."""
-    with _Call(x.device, stream) as call:
+    device = x.device
+    handle, context = _on(stream, device)
+    with context:
         args, keep = _softmax_args(x, w, targets, scale, offset)
-        ws, size = _softmax_workspace(args, False, call)
-        loss, lse = call.empty((args.n,), torch.float32), call.empty((args.n,), torch.float32)
-        _check(lib.ivfr_softmax_loss(ctypes.byref(args), _ptr(loss), _ptr(lse), _ptr(ws), size, call.handle))
+        ws, size = _softmax_workspace(args, 0, device)
+        loss, lse = torch.empty(args.n, device=device), torch.empty(args.n, device=device)
+        _check(lib.ivfr_softmax_loss(ctypes.byref(args), loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), size, handle))
     return loss, lse
 
 
 def softmax_loss_grad(x, w, targets, weight, scale=1.0, offset=None, lse=None, stream=None):
     """The gradients of sum_i weight_i loss_i.  weight: float32 [n].  Returns (loss, dx, dw), dx and dw of the inputs' type; with lse
     (of softmax_loss for the same arguments) given, the statistics are not formed again and loss is None."""
-    with _Call(x.device, stream) as call:
+    device = x.device
+    handle, context = _on(stream, device)
+    with context:
         args, keep = _softmax_args(x, w, targets, scale, offset)
         n, v, d = args.n, args.v, args.d
         for t, name in ((weight, "weight"), (lse, "lse")):
-            if t is not None and (t.shape != (n,) or t.dtype != torch.float32 or t.device != x.device):
+            if t is not None and (t.shape != (n,) or t.dtype != torch.float32 or t.device != device):
                 raise ValueError(f"{name} must be float32 [n] on the device of x")
         weight = weight.contiguous()
         lse = None if lse is None else lse.contiguous()
-        ws, size = _softmax_workspace(args, True, call)
-        loss = call.empty((n,), torch.float32) if lse is None else None
-        dx, dw = call.empty((n, d), x.dtype), call.empty((v, d), x.dtype)
-        _check(lib.ivfr_softmax_loss_grad(ctypes.byref(args), _ptr(weight), _ptr(lse), _ptr(loss), _ptr(dx), _ptr(dw), _ptr(ws), size,
-                                          call.handle))
+        ws, size = _softmax_workspace(args, 1, device)
+        loss = torch.empty(n, device=device) if lse is None else None
+        dx, dw = torch.empty((n, d), dtype=x.dtype, device=device), torch.empty((v, d), dtype=x.dtype, device=device)
+        _check(lib.ivfr_softmax_loss_grad(ctypes.byref(args), weight.data_ptr(), None if lse is None else lse.data_ptr(),
+                                          None if loss is None else loss.data_ptr(), dx.data_ptr(), dw.data_ptr(), ws.data_ptr(), size, handle))
     return loss, dx, dw
 
 
@@ -402,22 +394,25 @@ def orthogonalize(g, steps=5, coefficients=(3.4445, -4.7750, 2.0315), scale=1.0,
     The result is dense, of the shape and type of g."""
     if g.dim() not in (2, 3) or g.dtype not in _TYPES or not g.is_cuda:
         raise ValueError("g must be a float32, float16 or bfloat16 matrix, or a batch of them, on the GPU")
-    flat = [float(x) for k in coefficients for x in (k if hasattr(k, "__len__") else (k,))]
+    flat = [x for k in coefficients for x in (k if hasattr(k, "__len__") else (k,))]
     if len(flat) == 3:
-        flat = flat * int(steps)
-    if len(flat) != 3 * int(steps):
+        flat = flat * steps
+    if len(flat) != 3 * steps:
         raise ValueError("coefficients must be (a, b, c), or one such triple per step")
-    with _Call(g.device, stream) as call:
+    device = g.device
+    handle, context = _on(stream, device)
+    with context:
         m = g if g.dim() == 3 else g[None]
         b, rows, cols = m.shape
-        ld, each = m.stride(1) if rows > 1 else cols, m.stride(0) if b > 1 else rows * cols
-        if (cols > 1 and m.stride(2) != 1) or ld < cols or each < (rows - 1) * ld + cols:
+        each, ld, inner = m.stride()
+        ld, each = ld if rows > 1 else cols, each if b > 1 else rows * cols
+        if (cols > 1 and inner != 1) or ld < cols or (b > 1 and each < (rows - 1) * ld + cols):
             m, ld, each = m.contiguous(), cols, rows * cols
         coef = (ctypes.c_float * len(flat))(*flat)
-        args = OrthogonalizeArgs(b, rows, cols, _TYPES[g.dtype], int(steps), m.data_ptr(), ld, each, ctypes.cast(coef, ctypes.c_void_p),
-                                 float(scale), float(eps), g.device.index)
+        args = OrthogonalizeArgs(b, rows, cols, _TYPES[g.dtype], steps, m.data_ptr(), ld, each, ctypes.addressof(coef), scale, eps, device.index)
         need = ctypes.c_int64()
         _check(lib.ivfr_orthogonalize_workspace(ctypes.byref(args), ctypes.byref(need)))
-        ws, out = call.empty(need.value, torch.uint8), call.empty(tuple(g.shape), g.dtype)
-        _check(lib.ivfr_orthogonalize(ctypes.byref(args), _ptr(out), _ptr(ws), need.value, call.handle))
+        ws = torch.empty(need.value, dtype=torch.uint8, device=device)
+        out = torch.empty(g.shape, dtype=g.dtype, device=device)
+        _check(lib.ivfr_orthogonalize(ctypes.byref(args), out.data_ptr(), ws.data_ptr(), need.value, handle))
     return out

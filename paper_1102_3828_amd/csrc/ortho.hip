@@ -175,7 +175,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void gram_kernel(StepArg
     const uint32_t each = (uint32_t)a.tiles_p * (a.tiles_p + 1) / 2, total = each * (uint32_t)a.batch, per = (total + 7) / 8;
     const int64_t size = SQUARE ? a.asize : a.xsize;
     const uint16_t* const src0 = SQUARE ? a.in : a.x;
-    const ProductOperand operand = {src0, size, SQUARE ? a.ald : a.xld, a.rp, 0};
+    const ProductOperand operand = {src0, size, SQUARE ? a.ald : a.xld, a.rp, IVFR_PRODUCT_WHOLE};
     C::run(operand, operand, smem, [&](uint32_t i, ProductWork& w) {
         const uint32_t local = (blockIdx.x >> 3) + i * (gridDim.x >> 3), id = (blockIdx.x & 7) * per + local;
         if (local >= per || id >= total) return false;
@@ -231,7 +231,7 @@ typedef _Float16 half4v __attribute__((ext_vector_type(4)));
 template <class C>
 __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void update_kernel(StepArgs a) {
     __shared__ __align__(1024) char smem[C::LDS];
-    const ProductOperand P = {a.x, a.xsize, a.xld, a.cp, a.rp}, Q = {a.in, a.asize, a.ald, a.rp, 0};
+    const ProductOperand P = {a.x, a.xsize, a.xld, a.cp, a.rp}, Q = {a.in, a.asize, a.ald, a.rp, IVFR_PRODUCT_WHOLE};
     C::run(P, Q, smem, [&](uint32_t i, ProductWork& w) {
         if (!product_work(i, blockIdx.x, gridDim.x, a.tiles_p, a.tiles_q, a.batch, w)) return false;
         w.first = 0;
@@ -502,12 +502,22 @@ static int ortho_check(const ivfr_orthogonalize_args* a) {
     for (int s = 0; s < a->steps; ++s) {
         const double x = a->coefficients[3 * s], y = a->coefficients[3 * s + 1], z = a->coefficients[3 * s + 2];
         IVFR_REQUIRE(std::isfinite(x) && std::isfinite(y) && std::isfinite(z), "orthogonalize: the coefficients of step %d must be finite", s);
+        // the largest |v (x + w (y + w z))| and |w (y + w z)|, w = v^2, for v up to top: at the end or where a derivative is zero
         double next = 0.0, b = 0.0;
-        for (int i = 1; i <= 2048; ++i) {
-            const double v = top * i / 2048, w = v * v;
-            next = std::max(next, std::fabs(v * (x + w * (y + w * z))));
+        auto look = [&](double w) {
+            if (!(w > 0.0) || w > top * top) return;
+            next = std::max(next, std::sqrt(w) * std::fabs(x + w * (y + w * z)));
             b = std::max(b, std::fabs(w * (y + w * z)));
-        }
+        };
+        look(top * top);
+        const double root = 9.0 * y * y - 20.0 * x * z;   // of x + 3 y w + 5 z w^2
+        if (root >= 0.0)
+            for (double sign : {-1.0, 1.0}) {
+                const double q = -3.0 * y + sign * std::sqrt(root);   // (as q / 10 z and as 2 x / q: one of them without cancellation)
+                look(q / (10.0 * z));
+                look(2.0 * x / q);
+            }
+        look(-y / (2.0 * z));
         next *= 1.005;
         IVFR_REQUIRE(b < 15.0 && top * top < 15.0 && next < 15.0, "orthogonalize: the coefficients (%g, %g, %g) of step %d take singular values out of range (up to %g)", x, y, z, s, next);
         top = std::max(next, 1e-3);

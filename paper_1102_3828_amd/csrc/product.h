@@ -32,12 +32,13 @@ struct ProductOperand {
     int64_t plane;          // elements between planes
     int64_t ld;             // elements between rows, a multiple of 8
     int extent;             // values of the operand's own index; beyond it the last one (inner), or its last chunk of eight (outer), is read again
-    int rows;               // outer: rows of k that may be read; beyond them the last one is read again
+    int rows;               // k that may be read; beyond them the last row (outer) or chunk of eight (inner) is read again
     // Elements between panels of 256 of the inner axis.  256: rows lie whole.  A matrix kept in panels (ld 256) has its tiles in one piece each, where whole
     // rows of a hundred KB would spread a tile over as many pages as it has rows.
     int64_t panel = 256;
 };
 // Elements between the rows of an operand that is laid out here: whole lines of 128 bytes (with rows that begin inside a line every stage reads lines by halves: 8 % more time)
+#define IVFR_PRODUCT_WHOLE (1 << 30)   // rows, of an operand that is padded with zeros to whole slices
 inline int64_t product_ld(int64_t k) { return (k + 63) / 64 * 64; }
 
 // What a workgroup computes of a launch's tiles: the i-th tile of workgroup `block` of `blocks`.  XCDs take contiguous runs of tiles (blocks go round the
@@ -114,16 +115,17 @@ struct Product {
 
     // byte offset, from the operand's first row or column of this tile and the slice's first k, of what lane `lane` of load `i` of a plane brings
     template <bool OUTER, int SIZE, bool IS_P>
-    static __device__ __forceinline__ uint32_t source(int i, int lane, int64_t ld, int extent, int rows_left) {
+    static __device__ __forceinline__ uint32_t source(int i, int lane, int64_t ld, int extent, int k_left) {
         if constexpr (!OUTER) {
-            const int row = 16 * i + (lane >> 2);
-            const int chunk = (lane & 3) ^ (IS_P ? swz_p(row) : swz_q(row));
+            const int row = 16 * i + (lane >> 2), last = (k_left - 1) >> 3;
+            int chunk = (lane & 3) ^ (IS_P ? swz_p(row) : swz_q(row));
+            chunk = chunk < last ? chunk : last;   // (k_left of 32 or more: no change)
             return (uint32_t)(row < extent ? row : extent - 1) * (uint32_t)(2 * ld) + 16u * chunk;
         } else {
             constexpr int PER_ROW = SIZE / 8, ROWS = 64 / PER_ROW;
             const int k = ROWS * i + lane / PER_ROW, last = (extent - 1) >> 3;
             const int chunk = (lane % PER_ROW) ^ swz_k<SIZE>(k);
-            return (uint32_t)(k < rows_left ? k : rows_left - 1) * (uint32_t)(2 * ld) + 16u * (chunk < last ? chunk : last);
+            return (uint32_t)(k < k_left ? k : k_left - 1) * (uint32_t)(2 * ld) + 16u * (chunk < last ? chunk : last);
         }
     }
 
@@ -165,10 +167,8 @@ struct Product {
                 const int f = (wave + i * WAVES) % P_LOADS, row = f % P_ROWS, plane = f / P_ROWS % PLANES, sub = f / (P_ROWS * PLANES);
                 const int slice = ahead.first + (at + sub < ahead.count ? at + sub : ahead.count - 1);
                 uint32_t o = po[i % P_KINDS];
-                if constexpr (P_OUTER) {
-                    const int left = P.rows - slice * IVFR_PRODUCT_K;
-                    if (left < IVFR_PRODUCT_K) o = source<true, BM, true>(row, lane, P.ld, P.extent - ahead.p * BM, left);   // uniform
-                }
+                const int left = P.rows - slice * IVFR_PRODUCT_K;
+                if (left < IVFR_PRODUCT_K) o = source<P_OUTER, BM, true>(row, lane, P.ld, P.extent - ahead.p * BM, left);   // uniform
                 load16(base + sub * SLICE + plane * P_SLICE + 1024 * row, o, pn + slice_at(P, P_OUTER, slice) + (PLANES > 1 ? plane * P.plane : 0));
             }
 #pragma unroll
@@ -176,10 +176,8 @@ struct Product {
                 const int f = (wave + i * WAVES) % Q_LOADS, row = f % Q_ROWS, plane = f / Q_ROWS % PLANES, sub = f / (Q_ROWS * PLANES);
                 const int slice = ahead.first + (at + sub < ahead.count ? at + sub : ahead.count - 1);
                 uint32_t o = qo[i % Q_KINDS];
-                if constexpr (Q_OUTER) {
-                    const int left = Q.rows - slice * IVFR_PRODUCT_K;
-                    if (left < IVFR_PRODUCT_K) o = source<true, BN, false>(row, lane, Q.ld, Q.extent - ahead.q * BN, left);
-                }
+                const int left = Q.rows - slice * IVFR_PRODUCT_K;
+                if (left < IVFR_PRODUCT_K) o = source<Q_OUTER, BN, false>(row, lane, Q.ld, Q.extent - ahead.q * BN, left);
                 load16(base + sub * SLICE + PLANES * P_SLICE + plane * Q_SLICE + 1024 * row, o, qn + slice_at(Q, Q_OUTER, slice) + (PLANES > 1 ? plane * Q.plane : 0));
             }
             at += KSUB;
@@ -234,6 +232,14 @@ struct Product {
             for (int t = 0; t < TM; ++t) fp[t] = read_p(smem, 0, t);
             // slice number `sub` of its stage; `last` of its tile
             auto step = [&](int sub, bool last, short8v (&cq)[TN], short8v (&nq)[TN]) {
+                if constexpr (!Q_OUTER) {
+                    const int left = Q.rows - (w.first + w.count - 1) * IVFR_PRODUCT_K;
+                    if (last && left < IVFR_PRODUCT_K) {   // uniform; what was read past the end of k counts as zeros
+#pragma unroll
+                        for (int b = 0; b < TN; ++b)
+                            if (8 * g >= left) cq[b] = short8v{0, 0, 0, 0, 0, 0, 0, 0};
+                    }
+                }
                 const char* from = smem + buf * STAGE + (sub + 1) * SLICE;
                 if (sub + 1 == KSUB || last) {
                     wait_and_meet<(STAGES - 3) * EACH, (READS < 15 ? READS : 15)>();
@@ -343,22 +349,22 @@ struct Product {
 #define IVFR_TILE_256x256 0
 #define IVFR_TILE_128x128 1
 #define IVFR_TILE_64x64 2
-#define IVFR_TILE_256x64 3
-#define IVFR_TILE_256x16 4
+#define IVFR_TILE_128x64 3
+#define IVFR_TILE_128x16 4
 #define IVFR_TILES 5
-static const int IVFR_TILE_P[IVFR_TILES] = {256, 128, 64, 256, 256}, IVFR_TILE_Q[IVFR_TILES] = {256, 128, 64, 64, 16};
+static const int IVFR_TILE_P[IVFR_TILES] = {256, 128, 64, 128, 128}, IVFR_TILE_Q[IVFR_TILES] = {256, 128, 64, 64, 16};
 template <int TILE, bool PO, bool QO, bool HALF, int PLANES> struct ProductOf;
 template <bool PO, bool QO, bool HALF> struct ProductOf<0, PO, QO, HALF, 1> { typedef Product<256, 256, 2, 4, PO, QO, HALF, 1, 1, 4> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<1, PO, QO, HALF, 1> { typedef Product<128, 128, 2, 2, PO, QO, HALF, 1, 1, 4> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<2, PO, QO, HALF, 1> { typedef Product<64, 64, 2, 2, PO, QO, HALF, 1, 2, 4> T; };
-template <bool PO, bool QO, bool HALF> struct ProductOf<3, PO, QO, HALF, 1> { typedef Product<256, 64, 8, 1, PO, QO, HALF, 1, 1, 4> T; };
-template <bool PO, bool QO, bool HALF> struct ProductOf<4, PO, QO, HALF, 1> { typedef Product<256, 16, 8, 1, PO, QO, HALF, 1, 1, 4> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<3, PO, QO, HALF, 1> { typedef Product<128, 64, 4, 1, PO, QO, HALF, 1, 2, 3> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<4, PO, QO, HALF, 1> { typedef Product<128, 16, 4, 1, PO, QO, HALF, 1, 2, 4> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<1, PO, QO, HALF, 2> { typedef Product<128, 128, 2, 4, PO, QO, HALF, 2, 1, 4> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<2, PO, QO, HALF, 2> { typedef Product<64, 64, 2, 2, PO, QO, HALF, 2, 1, 4> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<1, PO, QO, HALF, 3> { typedef Product<128, 128, 2, 4, PO, QO, HALF, 3, 1, 3> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<2, PO, QO, HALF, 3> { typedef Product<64, 64, 2, 2, PO, QO, HALF, 3, 1, 3> T; };
-template <bool PO, bool QO, bool HALF> struct ProductOf<3, PO, QO, HALF, 3> { typedef Product<256, 64, 8, 1, PO, QO, HALF, 3, 1, 2> T; };
-template <bool PO, bool QO, bool HALF> struct ProductOf<4, PO, QO, HALF, 3> { typedef Product<256, 16, 8, 1, PO, QO, HALF, 3, 1, 3> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<3, PO, QO, HALF, 3> { typedef Product<128, 64, 4, 1, PO, QO, HALF, 3, 1, 2> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<4, PO, QO, HALF, 3> { typedef Product<128, 16, 4, 1, PO, QO, HALF, 3, 1, 3> T; };
 
 // rounding to nearest, ties to even
 __device__ __forceinline__ uint16_t to_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }

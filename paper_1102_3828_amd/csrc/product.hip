@@ -111,7 +111,7 @@ void product_cut(int64_t np, int64_t nq, int64_t slices, int planes, bool q_oute
     double least = 1e300;
     for (int k = 0; k < IVFR_TILES; ++k) {
         const int resident = COSTS[k].resident[planes - 1];
-        if (!resident || (k == IVFR_TILE_256x16 && (q_outer || nq > 64))) continue;
+        if (!resident || (k == IVFR_TILE_128x16 && (q_outer || nq > 64))) continue;
         const int64_t tiles = ((np + IVFR_TILE_P[k] - 1) / IVFR_TILE_P[k]) * ((nq + IVFR_TILE_Q[k] - 1) / IVFR_TILE_Q[k]);
         for (int s = 1; s <= 128 && s <= slices; s *= 2) {
             const int64_t per = (slices + s - 1) / s, parts = (slices + per - 1) / per, slots = (int64_t)IVFR_PRODUCT_CU * resident;
@@ -149,8 +149,8 @@ static int launch_tile(const ProductOut& o, hipStream_t st) {
             break;
         case IVFR_TILE_128x128: return launch_one<IVFR_TILE_128x128, QO, HALF, PLANES>(o, st);
         case IVFR_TILE_64x64: return launch_one<IVFR_TILE_64x64, QO, HALF, PLANES>(o, st);
-        case IVFR_TILE_256x16:
-            if constexpr (!QO) return launch_one<IVFR_TILE_256x16, false, HALF, PLANES>(o, st);
+        case IVFR_TILE_128x16:
+            if constexpr (!QO) return launch_one<IVFR_TILE_128x16, false, HALF, PLANES>(o, st);
             break;
     }
     ivfr_set_error("no such tile of a product: %d", o.tile);

@@ -243,10 +243,17 @@ __global__ __launch_bounds__(256) void loss_kernel(const float2* __restrict__ pa
     if (i >= n) return;   // uniform over a wavefront
     const float2* p = part + (int64_t)i * tiles;
     float m = -INFINITY, s = 0.f;
-    for (int t = lane; t < tiles; t += 64) {
-        const float2 x = p[t];
-        const float top = fmaxf(m, x.x), base = top == -INFINITY ? 0.f : top;
-        s = s * __builtin_amdgcn_exp2f(m - base) + x.y * __builtin_amdgcn_exp2f(x.x - base);
+    for (int t = lane; t < tiles; t += 64 * 8) {
+        float2 x[8];   // eight loads in flight
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = t + 64 * k < tiles ? p[t + 64 * k] : make_float2(-INFINITY, 0.f);
+        float top = m;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) top = fmaxf(top, x[k].x);
+        const float base = top == -INFINITY ? 0.f : top;
+        s *= __builtin_amdgcn_exp2f(m - base);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += x[k].y * __builtin_amdgcn_exp2f(x[k].x - base);
         m = top;
     }
 #pragma unroll
@@ -349,8 +356,8 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void grad_score_kernel(S
 
 // The tile by the sizes: few rows read the vectors once and are bound by that; else the largest tile that gives the compute units work.
 static int score_tile(int64_t n, int64_t v, int planes) {
-    if (n <= 16) return IVFR_TILE_256x16;
-    if (n <= 64) return IVFR_TILE_256x64;
+    if (n <= 16) return IVFR_TILE_128x16;
+    if (n <= 64) return IVFR_TILE_128x64;
     if (planes == 1 && ((n + 255) / 256) * ((v + 255) / 256) >= IVFR_PRODUCT_CU * 3 / 4) return IVFR_TILE_256x256;
     return ((n + 127) / 128) * ((v + 127) / 128) >= IVFR_PRODUCT_CU / 2 ? IVFR_TILE_128x128 : IVFR_TILE_64x64;
 }
@@ -372,8 +379,8 @@ static int launch_score_planes(const ScoreArgs& a, int tile, bool grad, hipStrea
             break;
         case IVFR_TILE_128x128: return launch_score_tile<IVFR_TILE_128x128, HALF, PLANES>(a, grad, st);
         case IVFR_TILE_64x64: return launch_score_tile<IVFR_TILE_64x64, HALF, PLANES>(a, grad, st);
-        case IVFR_TILE_256x64: return launch_score_tile<IVFR_TILE_256x64, HALF, PLANES>(a, grad, st);
-        case IVFR_TILE_256x16: return launch_score_tile<IVFR_TILE_256x16, HALF, PLANES>(a, grad, st);
+        case IVFR_TILE_128x64: return launch_score_tile<IVFR_TILE_128x64, HALF, PLANES>(a, grad, st);
+        case IVFR_TILE_128x16: return launch_score_tile<IVFR_TILE_128x16, HALF, PLANES>(a, grad, st);
     }
     ivfr_set_error("softmax: no such tile: %d", tile);
     return IVFR_ERR_INVALID_ARG;
@@ -422,8 +429,8 @@ static SoftmaxPlan softmax_plan(const ivfr_softmax_args& a, bool grad) {
     p.ld = product_ld(p.kd);
     p.n_pad = round_up(a.n, 32);
     // gradients read x by rows of k: padded to whole stages; rows that take no part are zeroed in the copy
-    p.pack_x = f32 || grad || a.d % 32 || !rows_aligned(a.x, a.ldx, 2);
-    p.pack_w = f32 || (grad && a.offset) || a.d % 32 || !rows_aligned(a.w, a.ldw, 2);
+    p.pack_x = f32 || grad || a.d % 8 || !rows_aligned(a.x, a.ldx, 2);
+    p.pack_w = f32 || (grad && a.offset) || a.d % 8 || !rows_aligned(a.w, a.ldw, 2);
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
         const int64_t here = at;
@@ -476,20 +483,20 @@ static int softmax_pointers(const ivfr_softmax_args& a, const SoftmaxPlan& p, co
 // weight: of a gradient, else null
 static int prepare(const ivfr_softmax_args& a, const SoftmaxPlan& p, const float* weight, char* ws, ScoreArgs& s, hipStream_t st) {
     const bool f32 = a.type == IVFR_TYPE_F32;
-    s.x = {(const uint16_t*)a.x, 0, a.ldx, (int)a.n, 0};
-    s.w = {(const uint16_t*)a.w, 0, a.ldw, (int)a.v, 0};
+    s.x = {(const uint16_t*)a.x, 0, a.ldx, (int)a.n, a.d};
+    s.w = {(const uint16_t*)a.w, 0, a.ldw, (int)a.v, a.d};
     PackArgs x = {}, w = {};
     UnitArgs u = {};
     auto blocks = [](const PackArgs& k) { return (unsigned)std::min<int64_t>((k.rows_out * (k.columns_out / 8) + 255) / 256, 4096); };
     if (p.pack_x) {
         x = {a.x, a.ldx, a.n, weight ? p.n_pad : a.n, p.kd, p.ld, a.d, rows_aligned(a.x, a.ldx, f32 ? 4 : 2), (uint16_t*)(ws + p.at_x), nullptr, weight ? a.targets : nullptr, 0};
         x.blocks = blocks(x);
-        s.x = {x.dst, x.rows_out * p.ld, p.ld, (int)x.rows_out, 0};   // (the rows of e reach up to the padding)
+        s.x = {x.dst, x.rows_out * p.ld, p.ld, (int)x.rows_out, IVFR_PRODUCT_WHOLE};   // (the rows of e reach up to the padding)
     }
     if (p.pack_w) {
         w = {a.w, a.ldw, a.v, a.v, p.kd, p.ld, a.d, rows_aligned(a.w, a.ldw, f32 ? 4 : 2), (uint16_t*)(ws + p.at_w), a.offset, nullptr, 0};
         w.blocks = blocks(w);
-        s.w = {w.dst, a.v * p.ld, p.ld, (int)a.v, 0};
+        s.w = {w.dst, a.v * p.ld, p.ld, (int)a.v, IVFR_PRODUCT_WHOLE};
     }
     if (weight && p.half) {
         u = {weight, a.targets, (int)a.n, (float*)(ws + p.at_unit)};
@@ -596,7 +603,7 @@ int ivfr_softmax_loss_grad(const ivfr_softmax_args* args, const float* weight, c
         ox.P = s.w;
         ox.P.extent = a.d;
         ox.P.rows = (int)here;
-        ox.Q = {s.e, p.e_plane, 256, (int)a.n, 0, p.n_pad * 256};
+        ox.Q = {s.e, p.e_plane, 256, (int)a.n, IVFR_PRODUCT_WHOLE, p.n_pad * 256};
         ox.slices = s.v_pad / 32;
         ox.nq = (int)a.n;
         ox.out = dx;
