@@ -357,7 +357,7 @@ template <int TILE, bool PO, bool QO, bool HALF, int PLANES> struct ProductOf;
 template <bool PO, bool QO, bool HALF> struct ProductOf<0, PO, QO, HALF, 1> { typedef Product<256, 256, 2, 4, PO, QO, HALF, 1, 1, 4> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<1, PO, QO, HALF, 1> { typedef Product<128, 128, 2, 2, PO, QO, HALF, 1, 1, 4> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<2, PO, QO, HALF, 1> { typedef Product<64, 64, 2, 2, PO, QO, HALF, 1, 2, 4> T; };
-template <bool PO, bool QO, bool HALF> struct ProductOf<3, PO, QO, HALF, 1> { typedef Product<128, 64, 4, 1, PO, QO, HALF, 1, 2, 3> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<3, PO, QO, HALF, 1> { typedef Product<128, 64, 4, 1, PO, QO, HALF, 1, 1, 4> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<4, PO, QO, HALF, 1> { typedef Product<128, 16, 4, 1, PO, QO, HALF, 1, 2, 4> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<1, PO, QO, HALF, 2> { typedef Product<128, 128, 2, 4, PO, QO, HALF, 2, 1, 4> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<2, PO, QO, HALF, 2> { typedef Product<64, 64, 2, 2, PO, QO, HALF, 2, 1, 4> T; };
