@@ -15,6 +15,8 @@
 #include <algorithm>
 #include <cmath>
 
+typedef _Float16 half4v __attribute__((ext_vector_type(4)));
+
 #define ORTHO_SCALE 4096.f
 #define ORTHO_SUMS 256         // workgroups at most that sum the squares of a matrix
 
@@ -225,8 +227,6 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void gram_kernel(StepArg
     }    });
 }
 
-typedef _Float16 half4v __attribute__((ext_vector_type(4)));
-
 // X <- first X + second B X
 template <class C>
 __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void update_kernel(StepArgs a) {
@@ -283,35 +283,51 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void update_kernel(StepA
 
 // All steps of a matrix in one workgroup, X and A (then B, in its place) in LDS: no launch and no memory in between.  A wavefront has
 // sixteen rows of the outputs and blocks of 32 of their columns (with fewer than 128 rows several wavefronts share the columns of the same rows), so
-// that it reads a fragment of its rows once for all blocks; results stay in registers until all have read what they replace.  Rows
-// in LDS are an odd number of 16-byte chunks long, so that the same chunk of sixteen rows lies in different banks.
+// that it reads a fragment of its rows once for all blocks; results stay in registers until all have read what they replace.
+// A matrix lies in LDS as slices of 32 columns, rows of 64 bytes, the four 16-byte chunks of a row permuted by its number: the lanes that are served together,
+// of eight rows (0-3 and 8-11: a wavefront's sixteen rows are every other four of 32) or, transposed, of four and four rows, meet different banks.
 #define SMALL_BLOCKS 8         // that a wavefront holds at most
 #define SMALL_WAVES 16
+#define SMALL_LDS 163584       // (of 163840; the sums of the norm beside it)
+#define SMALL_LDS_HALF 81664   // two workgroups on a compute unit
 
-__host__ __device__ inline int small_pitch(int k) { return 2 * k + 16; }   // bytes
 inline int small_blocks(int rp, int cp) { return (cp / 32 + SMALL_WAVES / (rp / 16) - 1) / (SMALL_WAVES / (rp / 16)); }   // of a wavefront
-inline int64_t small_lds(int rp, int cp, int planes) { return (int64_t)planes * rp * (small_pitch(cp) + small_pitch(rp)); }
+inline int64_t small_lds(int rp, int cp, int planes) { return (int64_t)planes * rp * (cp + rp) * 2; }
 
 struct SmallArgs {
     MatrixArgs m;
     float k[64][3];
     int steps;
 };
-
 struct Inner { static constexpr bool value = false; };   // how an operand lies
 struct Outer { static constexpr bool value = true; };
+
+// N values into their planes; two planes: the first one truncated (the second has what is left, to the nearest)
+template <int PLANES, int N>
+__device__ __forceinline__ void split_planes(const float (&v)[N], uint32_t (&h)[PLANES][N / 2]) {
+#pragma unroll
+    for (int e = 0; e < N; e += 2) {
+        if constexpr (PLANES == 1) h[0][e / 2] = to_half(v[e]) | (uint32_t)to_half(v[e + 1]) << 16;
+        else {
+            const auto top = __builtin_amdgcn_cvt_pkrtz(v[e], v[e + 1]);
+            h[0][e / 2] = __builtin_bit_cast(uint32_t, top);
+            h[1][e / 2] = to_half(fmaf((float)top[0], -1.f, v[e])) | (uint32_t)to_half(fmaf((float)top[1], -1.f, v[e + 1])) << 16;
+        }
+    }
+}
 
 template <int PLANES, int BLOCKS, int LDS>
 __global__ __launch_bounds__(64 * SMALL_WAVES, SMALL_WAVES / 4) void small_kernel(const SmallArgs a) {
     __shared__ __align__(16) char smem[LDS];
     __shared__ double red[SMALL_WAVES];
     MatrixArgs m = a.m;
-    const int rp = m.rp, cp = m.cp, xpitch = small_pitch(cp), apitch = small_pitch(rp);
-    const int xplane = rp * xpitch, aplane = rp * apitch;
+    const int rp = m.rp, cp = m.cp, slice = rp * 64, xplane = slice * (cp / 32), aplane = slice * (rp / 32);   // bytes
     char* const X = smem;
     char* const A = smem + PLANES * xplane;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int size = m.type == IVFR_TYPE_F32 ? 4 : 2;
+    auto swz = [](int row) { return ((row >> 1) & 1) | ((row >> 2) & 2); };
+    auto place = [&](int row, int k) { return (k >> 5) * slice + row * 64 + 16 * (((k >> 3) & 3) ^ swz(row)) + 2 * (k & 7); };
     m.g = (const char*)m.g + (int64_t)blockIdx.x * m.batch_stride * size;
     m.out = (char*)m.out + (int64_t)blockIdx.x * m.rows * m.cols * size;
     // the norm, then X; columns of g past the end are read as zeros, rows are padded here
@@ -337,42 +353,42 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, SMALL_WAVES / 4) void small_kerne
         float f[8];
         load_eight(m, row, k, f);
 #pragma unroll
-        for (int n = 0; n < PLANES; ++n) {
-            short8v h;
+        for (int e = 0; e < 8; ++e) f[e] = (float)(f[e] * inv);
+        uint32_t h[PLANES][4];
+        split_planes<PLANES>(f, h);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float v = n == 0 ? (float)(f[e] * inv) : f[e];
-                const uint16_t b = to_half(v);
-                h[e] = (short)b;
-                f[e] = v - from_half(b);
-            }
+        for (int n = 0; n < PLANES; ++n) {
             if (m.tall) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (k + e < m.cols) *reinterpret_cast<uint16_t*>(X + n * xplane + (k + e) * xpitch + 2 * row) = (uint16_t)h[e];
-            } else *reinterpret_cast<short8v*>(X + n * xplane + row * xpitch + 2 * k) = h;   // (the row is padded to 32 columns)
+                    if (k + e < m.cols) *reinterpret_cast<uint16_t*>(X + n * xplane + place(k + e, row)) = (uint16_t)(h[n][e / 2] >> (16 * (e & 1)));
+            } else *reinterpret_cast<uint4*>(X + n * xplane + place(row, k)) = make_uint4(h[n][0], h[n][1], h[n][2], h[n][3]);   // (the row is padded to 32 columns)
         }
     }
     __syncthreads();
     typedef Product<64, 64, 2, 2, false, false, true, 1, 1, 3> Unit;   // for its matrix instruction
-    // this wavefront's rows q0 .. q0 + 15 and blocks p0, p0 + 32 share, ...
-    const int rows16 = rp / 16, share = SMALL_WAVES / rows16, q0 = wave % rows16 * 16, p0 = wave / rows16 * 32;
+    // this wavefront's sixteen rows, every other four of 32, and its blocks p0, p0 + 32 share, ...
+    const int rows16 = rp / 16, share = SMALL_WAVES / rows16, qt = wave % rows16, p0 = wave / rows16 * 32;
     const bool idle = wave >= rows16 * share;
+    const int four = 8 * (r >> 2) + (r & 3), qrow = qt / 2 * 32 + 4 * (qt & 1) + four;
     auto blocks_of = [&](int columns) { return idle || p0 >= columns ? 0 : (columns - p0 - 1) / (32 * share) + 1; };
+    const uint32_t qplace = qrow * 64 + 16 * (g ^ swz(qrow));
     // acc[i] = the products of all planes for block i of n; the rows of P are columns of the output
-    auto form = [&](floatx4 (&acc)[BLOCKS][2], int n, const char* P, int ppitch, int pplane, auto p_outer, const char* Q, int qpitch, int qplane, int kn) {
+    auto form = [&](floatx4 (&acc)[BLOCKS][2], int n, const char* P, int pplane, auto p_outer, const char* Q, int qplane, int kn) {
         constexpr bool OUTER = decltype(p_outer)::value;
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i) acc[i][0] = acc[i][1] = floatx4{0.f, 0.f, 0.f, 0.f};
-        const uint32_t plane0 = OUTER ? (8 * g + (r >> 2)) * ppitch + 2 * (p0 + 4 * (r & 3)) : (p0 + r) * ppitch + 16 * g;
-        const int next = OUTER ? 64 * share : 32 * share * ppitch, half = OUTER ? 32 : 16 * ppitch, kstep = OUTER ? 32 * ppitch : 64;
         if (n == 0) return;   // uniform
+        // outer: row 8 g + (r >> 2) of k (and four further on), columns 16 t + 4 (r & 3); inner: rows `four` (and four further on), chunk g
+        const int krow = 8 * g + (r >> 2);
+        uint32_t place0 = OUTER ? p0 / 32 * slice + krow * 64 + 16 * (((r & 3) >> 1) ^ swz(krow)) + 8 * (r & 1) : (p0 + four) * 64 + 16 * (g ^ swz(four));
+        const int next = (OUTER ? slice : 2048) * share, kstep = OUTER ? 2048 : slice;
         for (int k = 0; k < kn; k += 32) {
-            uint32_t base = plane0 + k / 32 * kstep;
-            asm volatile("" : "+v"(base));   // (each block's address is one addition to this: not kept in registers over the steps)
+            uint32_t base = place0 + k / 32 * kstep;
+            asm volatile("" : "+v"(base));   // (a block's address is one addition to this: not kept in registers over the steps)
             short8v fq[PLANES];
 #pragma unroll
-            for (int z = 0; z < PLANES; ++z) fq[z] = *reinterpret_cast<const short8v*>(Q + z * qplane + (q0 + r) * qpitch + 2 * (k + 8 * g));
+            for (int z = 0; z < PLANES; ++z) fq[z] = *reinterpret_cast<const short8v*>(Q + z * qplane + qplace + k / 32 * slice);
 #pragma unroll
             for (int i = 0; i < BLOCKS; ++i) {
                 if (i >= n) break;   // uniform
@@ -381,14 +397,14 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, SMALL_WAVES / 4) void small_kerne
                 for (int z = 0; z < PLANES; ++z)
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
-                        const char* const b = P + z * pplane + i * next + t * half + base;
                         if constexpr (OUTER) {
+                            const char* const b = P + z * pplane + i * next + (base ^ (32 * t));
 #pragma unroll
                             for (int j = 0; j < 2; ++j) {
-                                const short4v h = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(b + 4 * j * ppitch));
+                                const short4v h = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(b + 256 * j));
                                 fp[z][t][4 * j] = h[0]; fp[z][t][4 * j + 1] = h[1]; fp[z][t][4 * j + 2] = h[2]; fp[z][t][4 * j + 3] = h[3];
                             }
-                        } else fp[z][t] = *reinterpret_cast<const short8v*>(b);
+                        } else fp[z][t] = *reinterpret_cast<const short8v*>(P + z * pplane + i * next + base + 256 * t);
                     }
 #pragma unroll
                 for (int sum = PLANES - 1; sum >= 0; --sum)
@@ -399,67 +415,66 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, SMALL_WAVES / 4) void small_kerne
             }
         }
     };
-    // four neighbouring values into their planes
-    auto put = [&](char* b, int plane, floatx4 v) {
+    // Block i of A: this lane has eight columns p0 + 8 g .. of row qrow, one chunk.  Block i of X: columns 16 t + 4 g .. + 3.
+    const uint32_t aplace = p0 / 32 * slice + qplace;
+    const uint32_t xplace = p0 / 32 * slice + qrow * 64 + 16 * ((g >> 1) ^ swz(qrow)) + 8 * (g & 1);   // t = 1: the other half of the row, ^ 32
+    auto put_a = [&](int i, const floatx4 (&o)[2]) {
+        float v[8] = {o[0][0], o[0][1], o[0][2], o[0][3], o[1][0], o[1][1], o[1][2], o[1][3]};
+        uint32_t h[PLANES][4];
+        split_planes<PLANES>(v, h);
 #pragma unroll
-        for (int n = 0; n < PLANES; ++n) {
-            short4v h;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint16_t x = to_half(v[e]);
-                h[e] = (short)x;
-                v[e] -= from_half(x);
-            }
-            *reinterpret_cast<short4v*>(b + n * plane) = h;
-        }
-    };
-    auto get = [&](const char* b, int plane) {
-        floatx4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int n = 0; n < PLANES; ++n) {
-            const short4v h = *reinterpret_cast<const short4v*>(b + n * plane);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += from_half((uint16_t)h[e]);
-        }
-        return v;
+        for (int z = 0; z < PLANES; ++z) *reinterpret_cast<uint4*>(A + z * aplane + aplace + i * share * slice) = make_uint4(h[z][0], h[z][1], h[z][2], h[z][3]);
     };
     const int an = blocks_of(rp), xn = blocks_of(cp);
-    const uint32_t aplace = (q0 + r) * apitch + 2 * (p0 + 4 * g), xplace = (q0 + r) * xpitch + 2 * (p0 + 4 * g);   // of this lane's outputs
     floatx4 out[BLOCKS][2];
     for (int step = 0; step < a.steps; ++step) {
         const float ka = a.k[step][0], kb = a.k[step][1], kc = a.k[step][2];
         // A = X X^T
-        form(out, an, X, xpitch, xplane, Inner(), X, xpitch, xplane, cp);
+        form(out, an, X, xplane, Inner(), X, xplane, cp);
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i) {
             if (i >= an) break;
 #pragma unroll
-            for (int t = 0; t < 2; ++t) put(A + aplace + 64 * share * i + 32 * t, aplane, out[i][t] * (1.f / ORTHO_SCALE));
+            for (int t = 0; t < 2; ++t) out[i][t] *= 1.f / ORTHO_SCALE;
+            put_a(i, out[i]);
         }
         __syncthreads();
         // B = b A + c A^2
-        form(out, an, A, apitch, aplane, Inner(), A, apitch, aplane, rp);
+        form(out, an, A, aplane, Inner(), A, aplane, rp);
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i) {
             if (i >= an) break;
 #pragma unroll
-            for (int t = 0; t < 2; ++t) out[i][t] = out[i][t] * (kc / ORTHO_SCALE) + get(A + aplace + 64 * share * i + 32 * t, aplane) * kb;
+            for (int t = 0; t < 2; ++t) out[i][t] *= kc / ORTHO_SCALE;
+#pragma unroll
+            for (int z = 0; z < PLANES; ++z) {
+                const half8v h = *reinterpret_cast<const half8v*>(A + z * aplane + aplace + i * share * slice);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) out[i][e >> 2][e & 3] = fmaf((float)h[e], kb, out[i][e >> 2][e & 3]);
+            }
         }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i) {
             if (i >= an) break;
-#pragma unroll
-            for (int t = 0; t < 2; ++t) put(A + aplace + 64 * share * i + 32 * t, aplane, out[i][t]);
+            put_a(i, out[i]);
         }
         __syncthreads();
         // X <- a X + B X
-        form(out, xn, X, xpitch, xplane, Outer(), A, apitch, aplane, rp);
+        form(out, xn, X, xplane, Outer(), A, aplane, rp);
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i) {
             if (i >= xn) break;
 #pragma unroll
-            for (int t = 0; t < 2; ++t) out[i][t] = out[i][t] * (1.f / ORTHO_SCALE) + get(X + xplace + 64 * share * i + 32 * t, xplane) * ka;
+            for (int t = 0; t < 2; ++t) {
+                out[i][t] *= 1.f / ORTHO_SCALE;
+#pragma unroll
+                for (int z = 0; z < PLANES; ++z) {
+                    const half4v h = *reinterpret_cast<const half4v*>(X + z * xplane + (xplace ^ (32 * t)) + i * share * slice);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) out[i][t][e] = fmaf((float)h[e], ka, out[i][t][e]);
+                }
+            }
         }
         if (step + 1 == a.steps) break;
         __syncthreads();
@@ -467,7 +482,13 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, SMALL_WAVES / 4) void small_kerne
         for (int i = 0; i < BLOCKS; ++i) {
             if (i >= xn) break;
 #pragma unroll
-            for (int t = 0; t < 2; ++t) put(X + xplace + 64 * share * i + 32 * t, xplane, out[i][t]);
+            for (int t = 0; t < 2; ++t) {
+                const float v[4] = {out[i][t][0], out[i][t][1], out[i][t][2], out[i][t][3]};
+                uint32_t h[PLANES][2];
+                split_planes<PLANES>(v, h);
+#pragma unroll
+                for (int z = 0; z < PLANES; ++z) *reinterpret_cast<uint2*>(X + z * xplane + (xplace ^ (32 * t)) + i * share * slice) = make_uint2(h[z][0], h[z][1]);
+            }
         }
         __syncthreads();
     }
@@ -478,7 +499,7 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, SMALL_WAVES / 4) void small_kerne
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int row = q0 + r, col = p0 + 32 * share * i + 16 * t + 4 * g + e, gr = m.tall ? col : row, gc = m.tall ? row : col;
+                const int col = p0 + 32 * share * i + 16 * t + 4 * g + e, gr = m.tall ? col : qrow, gc = m.tall ? qrow : col;
                 if (gr < m.rows && gc < m.cols) store_value(m.out, (int64_t)gr * m.cols + gc, m.type, out[i][t][e] * m.out_scale);
             }
     }
@@ -525,7 +546,6 @@ static int ortho_check(const ivfr_orthogonalize_args* a) {
     return IVFR_OK;
 }
 
-#define SMALL_LDS 163584       // (of 163840; the sums of the norm beside it)
 // Whether one workgroup a matrix is the faster way: a compute unit's products against 3 launches a step
 static bool small_pays(const OrthoPlan& p) {
     return true;
@@ -633,16 +653,18 @@ static int launch_small(const MatrixArgs& m, const ivfr_orthogonalize_args& a, h
     for (int i = 0; i < a.steps; ++i)
         for (int j = 0; j < 3; ++j) s.k[i][j] = a.coefficients[3 * i + j];
     const dim3 grid((unsigned)a.batch);
-    const bool half = small_lds(m.rp, m.cp, m.planes) <= 81664;   // two workgroups on a compute unit
-    const bool few = small_blocks(m.rp, m.cp) <= 2;
+    const bool half = small_lds(m.rp, m.cp, m.planes) <= SMALL_LDS_HALF;
+    const int blocks = small_blocks(m.rp, m.cp);
 #define IVFR_SMALL(PLANES, BLOCKS, LDS) hipLaunchKernelGGL((small_kernel<PLANES, BLOCKS, LDS>), grid, dim3(64 * SMALL_WAVES), 0, st, s)
     if (m.planes == 1) {
-        if (few) IVFR_SMALL(1, 2, 81664);   // (at most 128 x 128)
-        else if (half) IVFR_SMALL(1, SMALL_BLOCKS, 81664);
+        if (blocks <= 2) IVFR_SMALL(1, 2, SMALL_LDS_HALF);   // (at most 128 x 128)
+        else if (blocks <= 4 && half) IVFR_SMALL(1, 4, SMALL_LDS_HALF);
+        else if (blocks <= 4) IVFR_SMALL(1, 4, SMALL_LDS);
         else IVFR_SMALL(1, SMALL_BLOCKS, SMALL_LDS);
     } else {
-        if (few && half) IVFR_SMALL(2, 2, 81664);
-        else if (few) IVFR_SMALL(2, 2, SMALL_LDS);
+        if (blocks <= 2 && half) IVFR_SMALL(2, 2, SMALL_LDS_HALF);
+        else if (blocks <= 2) IVFR_SMALL(2, 2, SMALL_LDS);
+        else if (blocks <= 4) IVFR_SMALL(2, 4, SMALL_LDS);
         else IVFR_SMALL(2, SMALL_BLOCKS, SMALL_LDS);
     }
 #undef IVFR_SMALL
