@@ -33,7 +33,7 @@ struct MatrixArgs {
     const void* g;
     int64_t ld, batch_stride;
     int rows, cols, type;      // of g
-    int tall, rp, cp, xld, planes, vec;   // vec: rows start at 16-byte boundaries
+    int tall, rp, cp, xld, planes, align;   // align: of the rows, in bytes (16 at most)
     int64_t xsize;             // elements of a plane; a matrix has `planes` of them
     float eps;
     double* sums;              // [batch][parts]
@@ -69,35 +69,58 @@ __device__ __forceinline__ double sum_256(double s, double* red) {
     return red[0] + red[1] + red[2] + red[3];
 }
 
-// eight values of a row from column k (zeros past the end)
-__device__ __forceinline__ void load_eight(const MatrixArgs& a, int64_t row, int k, float (&f)[8]) {
-    const int64_t at = row * a.ld + k;
-    if (a.vec && k + 8 <= a.cols) {
-        if (a.type == IVFR_TYPE_F32) {
-            const float4 u = *reinterpret_cast<const float4*>((const float*)a.g + at), v = *reinterpret_cast<const float4*>((const float*)a.g + at + 4);
+// Eight values from element `at`, of which `left` exist (zeros for the others), by the widest loads that their alignment allows.
+template <bool F32>
+__device__ __forceinline__ void load_eight(const void* g, int64_t at, int align, int left, bool half, float (&f)[8]) {
+    if constexpr (F32) {
+        const float* p = (const float*)g + at;
+        if (left >= 8 && align >= 16) {
+            const float4 u = *reinterpret_cast<const float4*>(p), v = *reinterpret_cast<const float4*>(p + 4);
             f[0] = u.x; f[1] = u.y; f[2] = u.z; f[3] = u.w; f[4] = v.x; f[5] = v.y; f[6] = v.z; f[7] = v.w;
-        } else {
-            const short8v h = *reinterpret_cast<const short8v*>((const uint16_t*)a.g + at);
+        } else if (left >= 8) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = a.type == IVFR_TYPE_F16 ? from_half((uint16_t)h[e]) : from_bf16((uint16_t)h[e]);
+            for (int e = 0; e < 8; ++e) f[e] = p[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = e < left ? p[e] : 0.f;
         }
     } else {
+        const uint16_t* p = (const uint16_t*)g + at;
+        uint32_t h[4];
+        if (left >= 8 && align >= 16) {
+            const uint4 u = *reinterpret_cast<const uint4*>(p);
+            h[0] = u.x; h[1] = u.y; h[2] = u.z; h[3] = u.w;
+        } else if (left >= 8 && align >= 8) {
+            const uint2 u = *reinterpret_cast<const uint2*>(p), v = *reinterpret_cast<const uint2*>(p + 4);
+            h[0] = u.x; h[1] = u.y; h[2] = v.x; h[3] = v.y;
+        } else if (left >= 8 && align >= 4) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = k + e < a.cols ? load_value(a.g, at + e, a.type) : 0.f;
+            for (int e = 0; e < 4; ++e) h[e] = reinterpret_cast<const uint32_t*>(p)[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[e] = (2 * e < left ? p[2 * e] : 0u) | (2 * e + 1 < left ? (uint32_t)p[2 * e + 1] : 0u) << 16;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint16_t x = (uint16_t)(h[e / 2] >> (16 * (e & 1)));
+            f[e] = half ? from_half(x) : from_bf16(x);
+        }
     }
 }
 
 // Sums of squares, in fp64 (squares of fp32 values need not fit fp32), in a fixed order.  Bound by reading g.
+template <bool F32>
 __global__ __launch_bounds__(256) void squares_kernel(MatrixArgs a) {
     __shared__ double red[4];
-    a.g = (const char*)a.g + (int64_t)blockIdx.y * a.batch_stride * (a.type == IVFR_TYPE_F32 ? 4 : 2);
+    const int64_t base = (int64_t)blockIdx.y * a.batch_stride;
     const uint32_t chunks = (uint32_t)(a.cols + 7) / 8;
     const int64_t total = (int64_t)a.rows * chunks;
     double s = 0.0;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)a.parts * 256) {
         const int64_t row = total < (1ll << 32) ? (uint32_t)i / chunks : i / chunks;
+        const int k = (int)(i - row * chunks) * 8;
         float f[8];
-        load_eight(a, row, (int)(i - row * chunks) * 8, f);
+        load_eight<F32>(a.g, base + row * a.ld + k, a.align, a.cols - k, a.type == IVFR_TYPE_F16, f);
 #pragma unroll
         for (int e = 0; e < 8; ++e) s += (double)f[e] * f[e];
     }
@@ -330,39 +353,47 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, SMALL_WAVES / 4) void small_kerne
     auto place = [&](int row, int k) { return (k >> 5) * slice + row * 64 + 16 * (((k >> 3) & 3) ^ swz(row)) + 2 * (k & 7); };
     m.g = (const char*)m.g + (int64_t)blockIdx.x * m.batch_stride * size;
     m.out = (char*)m.out + (int64_t)blockIdx.x * m.rows * m.cols * size;
-    // the norm, then X; columns of g past the end are read as zeros, rows are padded here
+    // the norm, then X, of values that are read once; columns of g past the end are zeros, rows are padded here
+    constexpr bool F32 = PLANES > 1;
+    constexpr int HELD = F32 && BLOCKS > 5 ? 5 : BLOCKS;   // pieces of eight that a thread has at most: 4096 values a block, and what LDS holds
     const int chunks = (m.cols + 7) / 8, total = m.rows * chunks;
-    double s = 0.0;
-    for (int i = threadIdx.x; i < total; i += 64 * SMALL_WAVES) {
-        float f[8];
-        load_eight(m, i / chunks, i % chunks * 8, f);
+    float f[HELD][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s += (double)f[e] * f[e];
+    for (int h = 0; h < HELD; ++h) {
+        const int i = threadIdx.x + 64 * SMALL_WAVES * h, row = i / chunks, k = (i - row * chunks) * 8;
+        if (i < total) load_eight<F32>(m.g, (int64_t)row * m.ld + k, m.align, m.cols - k, m.type == IVFR_TYPE_F16, f[h]);
     }
+    for (int i = threadIdx.x; i < PLANES * xplane / 16; i += 64 * SMALL_WAVES) reinterpret_cast<uint4*>(X)[i] = make_uint4(0, 0, 0, 0);
+    double s = 0.0;
+#pragma unroll
+    for (int h = 0; h < HELD; ++h)
+        if ((int)threadIdx.x + 64 * SMALL_WAVES * h < total) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s += (double)f[h][e] * f[h][e];
+        }
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) s += __shfl_xor(s, off, 64);
     if (lane == 0) red[wave] = s;
-    for (int i = threadIdx.x; i < PLANES * xplane / 16; i += 64 * SMALL_WAVES) reinterpret_cast<uint4*>(X)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
     s = 0.0;
 #pragma unroll
     for (int w = 0; w < SMALL_WAVES; ++w) s += red[w];
     const double inv = (double)ORTHO_SCALE / (sqrt(s) + (double)m.eps);
-    for (int i = threadIdx.x; i < total; i += 64 * SMALL_WAVES) {
-        const int row = i / chunks, k = i % chunks * 8;
-        float f[8];
-        load_eight(m, row, k, f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = (float)(f[e] * inv);
-        uint32_t h[PLANES][4];
-        split_planes<PLANES>(f, h);
+    for (int h = 0; h < HELD; ++h) {
+        const int i = threadIdx.x + 64 * SMALL_WAVES * h, row = i / chunks, k = (i - row * chunks) * 8;
+        if (i >= total) continue;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[h][e] = (float)(f[h][e] * inv);
+        uint32_t b[PLANES][4];
+        split_planes<PLANES>(f[h], b);
 #pragma unroll
         for (int n = 0; n < PLANES; ++n) {
             if (m.tall) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (k + e < m.cols) *reinterpret_cast<uint16_t*>(X + n * xplane + place(k + e, row)) = (uint16_t)(h[n][e / 2] >> (16 * (e & 1)));
-            } else *reinterpret_cast<uint4*>(X + n * xplane + place(row, k)) = make_uint4(h[n][0], h[n][1], h[n][2], h[n][3]);   // (the row is padded to 32 columns)
+                    if (k + e < m.cols) *reinterpret_cast<uint16_t*>(X + n * xplane + place(k + e, row)) = (uint16_t)(b[n][e / 2] >> (16 * (e & 1)));
+            } else *reinterpret_cast<uint4*>(X + n * xplane + place(row, k)) = make_uint4(b[n][0], b[n][1], b[n][2], b[n][3]);   // (the row is padded to 32 columns)
         }
     }
     __syncthreads();
@@ -492,16 +523,32 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, SMALL_WAVES / 4) void small_kerne
         }
         __syncthreads();
     }
+    const bool four_at_once = !m.tall && m.cols % 4 == 0 && ((uintptr_t)m.out & (4 * size - 1)) == 0;   // uniform
 #pragma unroll
     for (int i = 0; i < BLOCKS; ++i) {
         if (i >= xn) break;
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 2; ++t) {
+            const int col = p0 + 32 * share * i + 16 * t + 4 * g;
+            const floatx4 v = out[i][t] * m.out_scale;
+            if (four_at_once) {
+                const int64_t at = (int64_t)qrow * m.cols + col;
+                if (qrow >= m.rows || col >= m.cols) continue;
+                if constexpr (F32) *reinterpret_cast<floatx4*>((float*)m.out + at) = v;
+                else {
+                    short4v h;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int col = p0 + 32 * share * i + 16 * t + 4 * g + e, gr = m.tall ? col : qrow, gc = m.tall ? qrow : col;
-                if (gr < m.rows && gc < m.cols) store_value(m.out, (int64_t)gr * m.cols + gc, m.type, out[i][t][e] * m.out_scale);
+                    for (int e = 0; e < 4; ++e) h[e] = (short)(m.type == IVFR_TYPE_F16 ? to_half(v[e]) : to_bf16(v[e]));
+                    *reinterpret_cast<short4v*>((uint16_t*)m.out + at) = h;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int gr = m.tall ? col + e : qrow, gc = m.tall ? qrow : col + e;
+                    if (gr < m.rows && gc < m.cols) store_value(m.out, (int64_t)gr * m.cols + gc, m.type, v[e]);
+                }
             }
+        }
     }
 }
 
@@ -546,11 +593,6 @@ static int ortho_check(const ivfr_orthogonalize_args* a) {
     return IVFR_OK;
 }
 
-// Whether one workgroup a matrix is the faster way: a compute unit's products against 3 launches a step
-static bool small_pays(const OrthoPlan& p) {
-    return true;
-}
-
 static OrthoPlan ortho_plan(const ivfr_orthogonalize_args& a) {
     OrthoPlan p = {};
     p.tall = a.rows > a.cols;
@@ -570,7 +612,8 @@ static OrthoPlan ortho_plan(const ivfr_orthogonalize_args& a) {
         at += round_up(bytes, 256);
         return here;
     };
-    p.small = small_lds(p.rp, p.cp, p.planes) <= SMALL_LDS && p.rp <= 128 && small_blocks(p.rp, p.cp) <= SMALL_BLOCKS && small_pays(p);
+    // (whatever fits: 128 x 128 in fp32 44 us against 91 in launches, 128 x 448 in bf16 88 against 88, 32 x 32 10 against 70)
+    p.small = small_lds(p.rp, p.cp, p.planes) <= SMALL_LDS && p.rp <= 128 && small_blocks(p.rp, p.cp) <= SMALL_BLOCKS;
     if (p.small) return p;
     p.parts = (int)std::min<int64_t>(ORTHO_SUMS, (p.xsize + 8191) / 8192);
     p.at_sums = take(p.batch * p.parts * 8);
@@ -687,9 +730,11 @@ int ivfr_orthogonalize(const ivfr_orthogonalize_args* args, void* out, void* wor
     char* const ws = (char*)workspace;
     MatrixArgs m = {a.g, a.ld, a.batch_stride, a.rows, a.cols, a.type, p.tall, p.rp, p.cp, p.xld, p.planes, 0, p.xsize, a.eps,
                     (double*)(ws + p.at_sums), p.parts, (uint16_t*)(ws + p.at_x[0]), out, a.scale / ORTHO_SCALE};
-    m.vec = ((uintptr_t)a.g & 15) == 0 && a.ld * size % 16 == 0 && (a.batch == 1 || a.batch_stride * size % 16 == 0);
+    m.align = 16;
+    while (((uintptr_t)a.g | (uintptr_t)(a.ld * size) | (uintptr_t)(a.batch > 1 ? a.batch_stride * size : 0)) & (m.align - 1)) m.align /= 2;
     if (p.small) return launch_small(m, a, st);
-    hipLaunchKernelGGL(squares_kernel, dim3((unsigned)p.parts, (unsigned)p.batch), dim3(256), 0, st, m);
+    if (a.type == IVFR_TYPE_F32) hipLaunchKernelGGL(squares_kernel<true>, dim3((unsigned)p.parts, (unsigned)p.batch), dim3(256), 0, st, m);
+    else hipLaunchKernelGGL(squares_kernel<false>, dim3((unsigned)p.parts, (unsigned)p.batch), dim3(256), 0, st, m);
     IVFR_HIP(hipGetLastError());
     const dim3 tiles((unsigned)((p.cp + 63) / 64), (unsigned)((p.rp + 63) / 64), (unsigned)p.batch);
     hipLaunchKernelGGL(fill_kernel, tiles, dim3(256), 0, st, m);
