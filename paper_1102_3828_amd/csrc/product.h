@@ -155,32 +155,50 @@ struct Product {
         };
         if (!work(loading, ahead)) return;   // uniform
         begin();
-        // The next stage goes to buffer `buf`.  Past the last slice of all tiles that one again, so that the number of loads in flight is always the same.
-        auto load = [&](int buf) {
+        // Where the next stage to load begins, found ahead of its loads (between the products, where the scalar unit has time).  Past the last slice of
+        // all tiles that one again, so that the number of loads in flight is always the same.
+        const uint16_t *pa[KSUB], *qa[KSUB];
+        int p_left = 0, q_left = 0;   // k from the stage's last slice on
+        auto prepare = [&]() {
             if (at >= ahead.count && more) {   // uniform
                 more = work(++loading, ahead);
                 if (more) begin();
             }
+            int slice = 0;
+#pragma unroll
+            for (int sub = 0; sub < KSUB; ++sub) {
+                slice = ahead.first + (at + sub < ahead.count ? at + sub : ahead.count - 1);
+                pa[sub] = pn + slice_at(P, P_OUTER, slice);
+                qa[sub] = qn + slice_at(Q, Q_OUTER, slice);
+            }
+            p_left = P.rows - slice * IVFR_PRODUCT_K;
+            q_left = Q.rows - slice * IVFR_PRODUCT_K;
+            at += KSUB;
+        };
+        auto load = [&](int buf) {
             const uint32_t base = lds0 + buf * STAGE;
+            const bool p_part = p_left < IVFR_PRODUCT_K, q_part = q_left < IVFR_PRODUCT_K;   // uniform
 #pragma unroll
             for (int i = 0; i < P_EACH; ++i) {
                 const int f = (wave + i * WAVES) % P_LOADS, row = f % P_ROWS, plane = f / P_ROWS % PLANES, sub = f / (P_ROWS * PLANES);
-                const int slice = ahead.first + (at + sub < ahead.count ? at + sub : ahead.count - 1);
                 uint32_t o = po[i % P_KINDS];
-                const int left = P.rows - slice * IVFR_PRODUCT_K;
-                if (left < IVFR_PRODUCT_K) o = source<P_OUTER, BM, true>(row, lane, P.ld, P.extent - ahead.p * BM, left);   // uniform
-                load16(base + sub * SLICE + plane * P_SLICE + 1024 * row, o, pn + slice_at(P, P_OUTER, slice) + (PLANES > 1 ? plane * P.plane : 0));
+                const uint16_t* from = pa[0];
+#pragma unroll
+                for (int z = 1; z < KSUB; ++z) from = sub == z ? pa[z] : from;
+                // (a slice before the last one of a stage is whole, or that one again)
+                if (p_part && (sub == KSUB - 1 || from == pa[KSUB - 1])) o = source<P_OUTER, BM, true>(row, lane, P.ld, P.extent - ahead.p * BM, p_left);
+                load16(base + sub * SLICE + plane * P_SLICE + 1024 * row, o, from + (PLANES > 1 ? plane * P.plane : 0));
             }
 #pragma unroll
             for (int i = 0; i < Q_EACH; ++i) {
                 const int f = (wave + i * WAVES) % Q_LOADS, row = f % Q_ROWS, plane = f / Q_ROWS % PLANES, sub = f / (Q_ROWS * PLANES);
-                const int slice = ahead.first + (at + sub < ahead.count ? at + sub : ahead.count - 1);
                 uint32_t o = qo[i % Q_KINDS];
-                const int left = Q.rows - slice * IVFR_PRODUCT_K;
-                if (left < IVFR_PRODUCT_K) o = source<Q_OUTER, BN, false>(row, lane, Q.ld, Q.extent - ahead.q * BN, left);
-                load16(base + sub * SLICE + PLANES * P_SLICE + plane * Q_SLICE + 1024 * row, o, qn + slice_at(Q, Q_OUTER, slice) + (PLANES > 1 ? plane * Q.plane : 0));
+                const uint16_t* from = qa[0];
+#pragma unroll
+                for (int z = 1; z < KSUB; ++z) from = sub == z ? qa[z] : from;
+                if (q_part && (sub == KSUB - 1 || from == qa[KSUB - 1])) o = source<Q_OUTER, BN, false>(row, lane, Q.ld, Q.extent - ahead.q * BN, q_left);
+                load16(base + sub * SLICE + PLANES * P_SLICE + plane * Q_SLICE + 1024 * row, o, from + (PLANES > 1 ? plane * Q.plane : 0));
             }
-            at += KSUB;
         };
         const int wm = wave / WAVES_N * (BM / WAVES_M), wn = wave % WAVES_N * (BN / WAVES_N);
         const int r = lane & 15, g = lane >> 4;
@@ -217,7 +235,11 @@ struct Product {
         floatx4 acc[TM][TN];
         ProductWork w;
 #pragma unroll
-        for (int s = 0; s < STAGES - 1; ++s) load(s);
+        for (int s = 0; s < STAGES - 1; ++s) {
+            prepare();
+            load(s);
+        }
+        prepare();
         int buf = 0;   // of the stage that is being used
         if constexpr (PLANES == 1) {
             // The fragments of a slice are read during the products of the slice before, each of P in place of the one that has just been used.
@@ -246,8 +268,8 @@ struct Product {
                     load(buf == 0 ? STAGES - 1 : buf - 1);
                     buf = buf + 1 == STAGES ? 0 : buf + 1;
                     from = smem + buf * STAGE;
+                    prepare();
                 }
-                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int a = 0; a < TM; ++a) {
 #pragma unroll
@@ -295,7 +317,6 @@ struct Product {
                 for (int s = 0; s < w.count; s += KSUB) {
                     // loaded are the stages up to the one after the next STAGES - 2
                     wait_and_meet<(STAGES - 2) * EACH, 0>();
-                    load(buf == 0 ? STAGES - 1 : buf - 1);   // (all have read the stage before)
 #pragma unroll
                     for (int sub = 0; sub < KSUB; ++sub) {
                         if (KSUB > 1 && s + sub >= w.count) break;   // uniform
@@ -308,6 +329,7 @@ struct Product {
 #pragma unroll
                             for (int t = 0; t < TM; ++t) fp[n][t] = read_p(from, n, t);
                         }
+                        if (sub == 0) load(buf == 0 ? STAGES - 1 : buf - 1);   // (all have read the stage before)
 #pragma unroll
                         for (int sum = PLANES - 1; sum >= 0; --sum)   // small products first
 #pragma unroll
@@ -317,6 +339,7 @@ struct Product {
 #pragma unroll
                                     for (int b = 0; b < TN; ++b) acc[a][b] = mfma(fp[n][a], fq[sum - n][b], acc[a][b]);
                     }
+                    prepare();
                     buf = buf + 1 == STAGES ? 0 : buf + 1;
                 }
                 done(w, acc);
