@@ -73,13 +73,15 @@ struct Product {
     static constexpr int PLANES = PLANES_, KSUB = KSUB_, STAGES = STAGES_;      // slices of 32 k in a stage, LDS buffers
     static constexpr bool P_OUTER = P_OUTER_, Q_OUTER = Q_OUTER_, HALF = HALF_;
     static constexpr int TM = BM / WAVES_M / 16, TN = BN / WAVES_N / 16;
-    static constexpr int KB = 2 * IVFR_PRODUCT_K;                               // bytes of a slice's k
-    static constexpr int P_SLICE = BM * KB, Q_SLICE = BN * KB, SLICE = (P_SLICE + Q_SLICE) * PLANES;
-    static constexpr int STAGE = SLICE * KSUB, LDS = STAGES * STAGE;
+    // Inner operands lie in LDS as rows of a stage's k, outer ones as rows of their own index.  With KSUB 2 a row of an inner operand brings 128 bytes, a
+    // whole line; with 64 the lines are fetched twice, by halves, and the L2 is what bounds the larger tiles.
+    static constexpr int ROW = 2 * IVFR_PRODUCT_K * KSUB, CHUNKS = ROW / 16;    // bytes and 16-byte chunks of such a row
+    static constexpr int P_BYTES = BM * ROW, Q_BYTES = BN * ROW;                // of a plane
+    static constexpr int STAGE = (P_BYTES + Q_BYTES) * PLANES, LDS = STAGES * STAGE;
     static constexpr int RESIDENT = 163840 / LDS >= 2 ? 2 : 1;                  // workgroups on a compute unit that registers are kept for
     static constexpr int WAVES_SIMD = WAVES * RESIDENT / 4 >= 1 ? WAVES * RESIDENT / 4 : 1;
-    static constexpr int P_ROWS = P_SLICE / 1024, Q_ROWS = Q_SLICE / 1024;      // loads of 64 lanes x 16 bytes for one plane of a slice
-    static constexpr int P_LOADS = P_ROWS * PLANES * KSUB, Q_LOADS = Q_ROWS * PLANES * KSUB;
+    static constexpr int P_ROWS = P_BYTES / 1024, Q_ROWS = Q_BYTES / 1024;      // loads of 64 lanes x 16 bytes for one plane of a stage
+    static constexpr int P_LOADS = P_ROWS * PLANES, Q_LOADS = Q_ROWS * PLANES;
     // Every wavefront issues the same number of loads, so that one count of those in flight holds for all (what is left over is
     // issued twice, the same bytes to the same place).
     static constexpr int P_EACH = (P_LOADS + WAVES - 1) / WAVES, Q_EACH = (Q_LOADS + WAVES - 1) / WAVES, EACH = P_EACH + Q_EACH;
@@ -90,13 +92,12 @@ struct Product {
     static_assert(P_OUTER || TM % 2 == 0, "");
     static_assert(!P_OUTER || BM >= 64, "");
     static_assert(!Q_OUTER || BN >= 64, "");
-    static_assert(EACH * (STAGES - 1) < 64 && LDS <= 163840, "");
-    static_assert(PLANES > 1 || ((KSUB == 1 || KSUB % 2 == 0) && STAGES >= 3), "");
+    static_assert(EACH * (STAGES - 1) < 64 && LDS <= 163840 && STAGES >= 2 && (KSUB == 1 || KSUB == 2), "");
 
-    // permutation of the chunks of a row in LDS: inner rows have four of them
-    static __device__ __forceinline__ int swz_p(int row) { return ((row >> 1) & 1) | ((row >> 2) & 2); }   // rows 0-3, 8-11 together
-    static __device__ __forceinline__ int swz_q(int row) { return (row >> 1) & 3; }                        // rows 0-7 together
-    // rows of k, of SIZE columns: two lane groups read 32 bytes of four rows each (k..k + 3, k + 8..k + 11) together, from 256 bytes of banks
+    // permutation of the chunks of a row in LDS: of inner rows 0-3, 8-11 together (P) or 0-7 (Q)
+    static __device__ __forceinline__ int swz_p(int row) { return KSUB == 1 ? ((row >> 1) & 1) | ((row >> 2) & 2) : (row & 3) | ((row >> 1) & 4); }
+    static __device__ __forceinline__ int swz_q(int row) { return KSUB == 1 ? (row >> 1) & 3 : row & 7; }
+    // of rows of k, of SIZE columns: two lane groups read 32 bytes of four rows each (k..k + 3, k + 8..k + 11) together, from 256 bytes of banks
     template <int SIZE>
     static __device__ __forceinline__ int swz_k(int k) { return SIZE == 64 ? (k & 2) | ((k >> 1) & 4) : ((k & 3) << 1) | (k & 8); }
 
@@ -113,13 +114,14 @@ struct Product {
         else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     }
 
-    // byte offset, from the operand's first row or column of this tile and the slice's first k, of what lane `lane` of load `i` of a plane brings
+    // Byte offset, from the operand's first row or column of this tile and the stage's first k, of what lane `lane` of load `i` of a plane brings.
+    // k_left: what there is of k from there; past it the last chunk (inner) or row (outer) again.
     template <bool OUTER, int SIZE, bool IS_P>
     static __device__ __forceinline__ uint32_t source(int i, int lane, int64_t ld, int extent, int k_left) {
         if constexpr (!OUTER) {
-            const int row = 16 * i + (lane >> 2), last = (k_left - 1) >> 3;
-            int chunk = (lane & 3) ^ (IS_P ? swz_p(row) : swz_q(row));
-            chunk = chunk < last ? chunk : last;   // (k_left of 32 or more: no change)
+            const int row = 64 / CHUNKS * i + lane / CHUNKS, last = (k_left - 1) >> 3;
+            int chunk = (lane % CHUNKS) ^ (IS_P ? swz_p(row) : swz_q(row));
+            chunk = chunk < last ? chunk : last;
             return (uint32_t)(row < extent ? row : extent - 1) * (uint32_t)(2 * ld) + 16u * chunk;
         } else {
             constexpr int PER_ROW = SIZE / 8, ROWS = 64 / PER_ROW;
@@ -149,55 +151,44 @@ struct Product {
             qn = Q.base + ahead.q_at + (Q_OUTER ? (q0 >> 8) * Q.panel + (q0 & 255) : q0 * Q.ld);
             at = 0;
 #pragma unroll
-            for (int i = 0; i < P_KINDS; ++i) po[i] = source<P_OUTER, BM, true>((wave + i * WAVES) % P_ROWS, lane, P.ld, P.extent - p0, IVFR_PRODUCT_K);
+            for (int i = 0; i < P_KINDS; ++i) po[i] = source<P_OUTER, BM, true>((wave + i * WAVES) % P_ROWS, lane, P.ld, P.extent - p0, IVFR_PRODUCT_K * KSUB);
 #pragma unroll
-            for (int i = 0; i < Q_KINDS; ++i) qo[i] = source<Q_OUTER, BN, false>((wave + i * WAVES) % Q_ROWS, lane, Q.ld, Q.extent - q0, IVFR_PRODUCT_K);
+            for (int i = 0; i < Q_KINDS; ++i) qo[i] = source<Q_OUTER, BN, false>((wave + i * WAVES) % Q_ROWS, lane, Q.ld, Q.extent - q0, IVFR_PRODUCT_K * KSUB);
         };
         if (!work(loading, ahead)) return;   // uniform
         begin();
-        // Where the next stage to load begins, found ahead of its loads (between the products, where the scalar unit has time).  Past the last slice of
+        // Where the next stage to load begins, found ahead of its loads (among the products, where the scalar unit has time).  Past the last stage of
         // all tiles that one again, so that the number of loads in flight is always the same.
-        const uint16_t *pa[KSUB], *qa[KSUB];
-        int p_left = 0, q_left = 0;   // k from the stage's last slice on
+        const uint16_t *pa, *qa;
+        int p_left = 0, q_left = 0;   // k from there on
         auto prepare = [&]() {
             if (at >= ahead.count && more) {   // uniform
                 more = work(++loading, ahead);
                 if (more) begin();
             }
-            int slice = 0;
-#pragma unroll
-            for (int sub = 0; sub < KSUB; ++sub) {
-                slice = ahead.first + (at + sub < ahead.count ? at + sub : ahead.count - 1);
-                pa[sub] = pn + slice_at(P, P_OUTER, slice);
-                qa[sub] = qn + slice_at(Q, Q_OUTER, slice);
-            }
+            const int slice = ahead.first + (at < ahead.count ? at : (ahead.count - 1) / KSUB * KSUB);
+            pa = pn + slice_at(P, P_OUTER, slice);
+            qa = qn + slice_at(Q, Q_OUTER, slice);
             p_left = P.rows - slice * IVFR_PRODUCT_K;
             q_left = Q.rows - slice * IVFR_PRODUCT_K;
             at += KSUB;
         };
         auto load = [&](int buf) {
             const uint32_t base = lds0 + buf * STAGE;
-            const bool p_part = p_left < IVFR_PRODUCT_K, q_part = q_left < IVFR_PRODUCT_K;   // uniform
+            const bool p_part = p_left < IVFR_PRODUCT_K * KSUB, q_part = q_left < IVFR_PRODUCT_K * KSUB;   // uniform
 #pragma unroll
             for (int i = 0; i < P_EACH; ++i) {
-                const int f = (wave + i * WAVES) % P_LOADS, row = f % P_ROWS, plane = f / P_ROWS % PLANES, sub = f / (P_ROWS * PLANES);
+                const int f = (wave + i * WAVES) % P_LOADS, row = f % P_ROWS, plane = f / P_ROWS;
                 uint32_t o = po[i % P_KINDS];
-                const uint16_t* from = pa[0];
-#pragma unroll
-                for (int z = 1; z < KSUB; ++z) from = sub == z ? pa[z] : from;
-                // (a slice before the last one of a stage is whole, or that one again)
-                if (p_part && (sub == KSUB - 1 || from == pa[KSUB - 1])) o = source<P_OUTER, BM, true>(row, lane, P.ld, P.extent - ahead.p * BM, p_left);
-                load16(base + sub * SLICE + plane * P_SLICE + 1024 * row, o, from + (PLANES > 1 ? plane * P.plane : 0));
+                if (p_part) o = source<P_OUTER, BM, true>(row, lane, P.ld, P.extent - ahead.p * BM, p_left);
+                load16(base + plane * P_BYTES + 1024 * row, o, pa + (PLANES > 1 ? plane * P.plane : 0));
             }
 #pragma unroll
             for (int i = 0; i < Q_EACH; ++i) {
-                const int f = (wave + i * WAVES) % Q_LOADS, row = f % Q_ROWS, plane = f / Q_ROWS % PLANES, sub = f / (Q_ROWS * PLANES);
+                const int f = (wave + i * WAVES) % Q_LOADS, row = f % Q_ROWS, plane = f / Q_ROWS;
                 uint32_t o = qo[i % Q_KINDS];
-                const uint16_t* from = qa[0];
-#pragma unroll
-                for (int z = 1; z < KSUB; ++z) from = sub == z ? qa[z] : from;
-                if (q_part && (sub == KSUB - 1 || from == qa[KSUB - 1])) o = source<Q_OUTER, BN, false>(row, lane, Q.ld, Q.extent - ahead.q * BN, q_left);
-                load16(base + sub * SLICE + PLANES * P_SLICE + plane * Q_SLICE + 1024 * row, o, from + (PLANES > 1 ? plane * Q.plane : 0));
+                if (q_part) o = source<Q_OUTER, BN, false>(row, lane, Q.ld, Q.extent - ahead.q * BN, q_left);
+                load16(base + PLANES * P_BYTES + plane * Q_BYTES + 1024 * row, o, qa + (PLANES > 1 ? plane * Q.plane : 0));
             }
         };
         const int wm = wave / WAVES_N * (BM / WAVES_M), wn = wave % WAVES_N * (BN / WAVES_N);
@@ -208,8 +199,8 @@ struct Product {
         for (int j = 0; j < 2; ++j) {
             // outer: the row of k (the column's chunk comes with the tile)
             const int row = wm + 8 * (r >> 2) + 4 * j + (r & 3), k = 8 * g + 4 * j + (r >> 2);
-            pf[j] = P_OUTER ? k * (2 * BM) : row * KB + 16 * (g ^ swz_p(row));
-            qf[j] = Q_OUTER ? k * (2 * BN) : (wn + r) * KB + 16 * (g ^ swz_q(wn + r));
+            pf[j] = P_OUTER ? k * (2 * BM) : row * ROW + 16 * (g ^ swz_p(row));
+            qf[j] = Q_OUTER ? k * (2 * BN) : (wn + r) * ROW + 16 * (g ^ swz_q(wn + r));
         }
         auto outer_read = [&](const char* b, const uint32_t (&rows)[2], int column, int swizzle) {   // eight k of column + (l & 15)
             short8v v;
@@ -222,20 +213,22 @@ struct Product {
             return v;
         };
         const int pk = swz_k<BM>(8 * g + (r >> 2)), qk = swz_k<BN>(8 * g + (r >> 2));   // (the same four rows further on)
-        auto read_p = [&](const char* slice, int plane, int t) {
-            const char* const b = slice + plane * P_SLICE;
-            if constexpr (P_OUTER) return outer_read(b, pf, wm + 16 * t, pk);
-            else return *reinterpret_cast<const short8v*>(b + pf[t & 1] + (t >> 1) * 32 * KB);
+        // fragments of slice `sub` of a stage
+        auto read_p = [&](const char* stage, int sub, int plane, int t) {
+            const char* const b = stage + plane * P_BYTES;
+            if constexpr (P_OUTER) return outer_read(b + sub * (2 * BM * IVFR_PRODUCT_K), pf, wm + 16 * t, pk);
+            else return *reinterpret_cast<const short8v*>(b + (pf[t & 1] ^ (64 * sub)) + (t >> 1) * 32 * ROW);
         };
-        auto read_q = [&](const char* slice, int plane, int t) {
-            const char* const b = slice + PLANES * P_SLICE + plane * Q_SLICE;
-            if constexpr (Q_OUTER) return outer_read(b, qf, wn + 16 * t, qk);
-            else return *reinterpret_cast<const short8v*>(b + qf[0] + t * 16 * KB);
+        auto read_q = [&](const char* stage, int sub, int plane, int t) {
+            const char* const b = stage + PLANES * P_BYTES + plane * Q_BYTES;
+            if constexpr (Q_OUTER) return outer_read(b + sub * (2 * BN * IVFR_PRODUCT_K), qf, wn + 16 * t, qk);
+            else return *reinterpret_cast<const short8v*>(b + (qf[0] ^ (64 * sub)) + t * 16 * ROW);
         };
         floatx4 acc[TM][TN];
         ProductWork w;
+        constexpr int AHEAD = PLANES == 1 ? STAGES : STAGES - 1;   // stages loaded before the first one is used
 #pragma unroll
-        for (int s = 0; s < STAGES - 1; ++s) {
+        for (int s = 0; s < AHEAD; ++s) {
             prepare();
             load(s);
         }
@@ -243,15 +236,15 @@ struct Product {
         int buf = 0;   // of the stage that is being used
         if constexpr (PLANES == 1) {
             // The fragments of a slice are read during the products of the slice before, each of P in place of the one that has just been used.
-            // At the start of stage s all wavefronts are done with the reads of stage s - 1 (each has at most those of one slice
-            // outstanding, of stage s), so that its buffer is loaded with stage s + STAGES - 1; stages up to s + STAGES - 2 were loaded before, and s + 1 is needed.
-            constexpr int P_READS = P_OUTER ? 2 : 1, Q_READS = Q_OUTER ? 2 : 1, READS = P_READS * TM + Q_READS * TN;
+            // Before the last slice of stage s all wavefronts have read all of s, so that its buffer is loaded with stage s + STAGES; the stages before that
+            // are on their way, and s + 1 is needed.
+            constexpr int P_READS = P_OUTER ? 2 : 1, Q_READS = Q_OUTER ? 2 : 1;
             short8v fp[TM], fq[2][TN];
-            wait_and_meet<(STAGES - 2) * EACH, 0>();
+            wait_and_meet<(STAGES - 1) * EACH, 0>();
 #pragma unroll
-            for (int t = 0; t < TN; ++t) fq[0][t] = read_q(smem, 0, t);
+            for (int t = 0; t < TN; ++t) fq[0][t] = read_q(smem, 0, 0, t);
 #pragma unroll
-            for (int t = 0; t < TM; ++t) fp[t] = read_p(smem, 0, t);
+            for (int t = 0; t < TM; ++t) fp[t] = read_p(smem, 0, 0, t);
             // slice number `sub` of its stage; `last` of its tile
             auto step = [&](int sub, bool last, short8v (&cq)[TN], short8v (&nq)[TN]) {
                 if constexpr (!Q_OUTER) {
@@ -262,21 +255,23 @@ struct Product {
                             if (8 * g >= left) cq[b] = short8v{0, 0, 0, 0, 0, 0, 0, 0};
                     }
                 }
-                const char* from = smem + buf * STAGE + (sub + 1) * SLICE;
+                int next = sub + 1;
                 if (sub + 1 == KSUB || last) {
-                    wait_and_meet<(STAGES - 3) * EACH, (READS < 15 ? READS : 15)>();
-                    load(buf == 0 ? STAGES - 1 : buf - 1);
+                    wait_and_meet<(STAGES - 2) * EACH, 0>();
+                    load(buf);
                     buf = buf + 1 == STAGES ? 0 : buf + 1;
-                    from = smem + buf * STAGE;
+                    next = 0;
                     prepare();
                 }
+                const char* const from = smem + buf * STAGE;
+                const int nsub = sub + 1 == KSUB ? 0 : next;   // (known when compiled where a stage has one slice, or this is its last)
 #pragma unroll
                 for (int a = 0; a < TM; ++a) {
 #pragma unroll
                     for (int b = 0; b < TN; ++b) acc[a][b] = mfma(fp[a], cq[b], acc[a][b]);
-                    fp[a] = read_p(from, 0, a);
+                    fp[a] = read_p(from, nsub, 0, a);
 #pragma unroll
-                    for (int b = a * TN / TM; b < (a + 1) * TN / TM; ++b) nq[b] = read_q(from, 0, b);
+                    for (int b = a * TN / TM; b < (a + 1) * TN / TM; ++b) nq[b] = read_q(from, nsub, 0, b);
                 }
 #pragma unroll
                 for (int a = 0; a < TM; ++a) {
@@ -320,14 +315,14 @@ struct Product {
 #pragma unroll
                     for (int sub = 0; sub < KSUB; ++sub) {
                         if (KSUB > 1 && s + sub >= w.count) break;   // uniform
-                        const char* const from = smem + buf * STAGE + sub * SLICE;
+                        const char* const from = smem + buf * STAGE;
                         short8v fp[PLANES][TM], fq[PLANES][TN];
 #pragma unroll
                         for (int n = PLANES - 1; n >= 0; --n) {
 #pragma unroll
-                            for (int t = 0; t < TN; ++t) fq[n][t] = read_q(from, n, t);
+                            for (int t = 0; t < TN; ++t) fq[n][t] = read_q(from, sub, n, t);
 #pragma unroll
-                            for (int t = 0; t < TM; ++t) fp[n][t] = read_p(from, n, t);
+                            for (int t = 0; t < TM; ++t) fp[n][t] = read_p(from, sub, n, t);
                         }
                         if (sub == 0) load(buf == 0 ? STAGES - 1 : buf - 1);   // (all have read the stage before)
 #pragma unroll
@@ -377,12 +372,12 @@ struct Product {
 #define IVFR_TILES 5
 static const int IVFR_TILE_P[IVFR_TILES] = {256, 128, 64, 128, 128}, IVFR_TILE_Q[IVFR_TILES] = {256, 128, 64, 64, 16};
 template <int TILE, bool PO, bool QO, bool HALF, int PLANES> struct ProductOf;
-template <bool PO, bool QO, bool HALF> struct ProductOf<0, PO, QO, HALF, 1> { typedef Product<256, 256, 2, 4, PO, QO, HALF, 1, 1, 4> T; };
-template <bool PO, bool QO, bool HALF> struct ProductOf<1, PO, QO, HALF, 1> { typedef Product<128, 128, 2, 2, PO, QO, HALF, 1, 1, 4> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<0, PO, QO, HALF, 1> { typedef Product<256, 256, 2, 4, PO, QO, HALF, 1, 2, 2> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<1, PO, QO, HALF, 1> { typedef Product<128, 128, 2, 2, PO, QO, HALF, 1, 2, 2> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<2, PO, QO, HALF, 1> { typedef Product<64, 64, 2, 2, PO, QO, HALF, 1, 2, 4> T; };
-template <bool PO, bool QO, bool HALF> struct ProductOf<3, PO, QO, HALF, 1> { typedef Product<128, 64, 4, 1, PO, QO, HALF, 1, 1, 4> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<3, PO, QO, HALF, 1> { typedef Product<128, 64, 4, 1, PO, QO, HALF, 1, 2, 3> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<4, PO, QO, HALF, 1> { typedef Product<128, 16, 4, 1, PO, QO, HALF, 1, 2, 4> T; };
-template <bool PO, bool QO, bool HALF> struct ProductOf<1, PO, QO, HALF, 2> { typedef Product<128, 128, 2, 4, PO, QO, HALF, 2, 1, 4> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<1, PO, QO, HALF, 2> { typedef Product<128, 128, 2, 4, PO, QO, HALF, 2, 2, 2> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<2, PO, QO, HALF, 2> { typedef Product<64, 64, 2, 2, PO, QO, HALF, 2, 1, 4> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<1, PO, QO, HALF, 3> { typedef Product<128, 128, 2, 4, PO, QO, HALF, 3, 1, 3> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<2, PO, QO, HALF, 3> { typedef Product<64, 64, 2, 2, PO, QO, HALF, 3, 1, 3> T; };
@@ -415,6 +410,8 @@ struct ProductOut {            // out[q][p] = alpha * unit * sum_k P(p, k) Q(q, 
 };
 // The tile and the number of parts of k for a product of these sizes; q_outer: Q too.
 void product_cut(int64_t np, int64_t nq, int64_t slices, int planes, bool q_outer, int* tile, int* splits);
+// slices of a part: whole stages
+__host__ __device__ inline int product_per(int slices, int splits) { return ((slices + splits - 1) / splits + 1) / 2 * 2; }
 inline int64_t product_pad(int64_t np) { return (np + 3) / 4 * 4; }
 // x: Q inner; w: Q outer.  Both in one launch where their tiles are the same small ones.
 int product_launch(const ProductOut& x, const ProductOut& w, bool half, hipStream_t st);

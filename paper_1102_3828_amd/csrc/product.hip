@@ -27,7 +27,7 @@ __device__ __forceinline__ void store_four(void* out, int64_t at, int type, cons
 
 template <class C>
 __device__ __forceinline__ void form(const ProductOut& o, uint32_t block, uint32_t blocks, char* smem) {
-    const int tiles_p = (o.np + C::BM - 1) / C::BM, tiles_q = (o.nq + C::BN - 1) / C::BN, per = (o.slices + o.splits - 1) / o.splits;
+    const int tiles_p = (o.np + C::BM - 1) / C::BM, tiles_q = (o.nq + C::BN - 1) / C::BN, per = product_per(o.slices, o.splits);
     const float alpha = o.partial ? 1.f : o.alpha * (o.unit ? o.unit[1] : 1.f);
     const int64_t ld = o.partial ? (o.np + 3) / 4 * 4 : o.ld;
     const int type = o.partial ? IVFR_TYPE_F32 : o.type, limit = o.partial ? (int)ld : o.np;
@@ -114,7 +114,7 @@ void product_cut(int64_t np, int64_t nq, int64_t slices, int planes, bool q_oute
         if (!resident || (k == IVFR_TILE_128x16 && (q_outer || nq > 64))) continue;
         const int64_t tiles = ((np + IVFR_TILE_P[k] - 1) / IVFR_TILE_P[k]) * ((nq + IVFR_TILE_Q[k] - 1) / IVFR_TILE_Q[k]);
         for (int s = 1; s <= 128 && s <= slices; s *= 2) {
-            const int64_t per = (slices + s - 1) / s, parts = (slices + per - 1) / per, slots = (int64_t)IVFR_PRODUCT_CU * resident;
+            const int64_t per = product_per((int)slices, s), parts = (slices + per - 1) / per, slots = (int64_t)IVFR_PRODUCT_CU * resident;
             const double rounds = (double)((tiles * parts + slots - 1) / slots);
             // (workgroups that share a compute unit share its matrix units)
             const double share = tiles * parts <= IVFR_PRODUCT_CU ? 0.6 : 1.0;

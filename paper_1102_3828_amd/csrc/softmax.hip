@@ -581,7 +581,7 @@ int ivfr_softmax_loss_grad(const ivfr_softmax_args* args, const float* weight, c
     ProductOut ox = {}, ow = {};
     int slots = 0;
     // (the last piece may have too few slices for as many parts)
-    auto parts_of = [](int slices, int splits) { const int per = (slices + splits - 1) / splits; return (slices + per - 1) / per; };
+    auto parts_of = [](int slices, int splits) { const int per = product_per(slices, splits); return (slices + per - 1) / per; };
     for (int i = 0; i < p.pieces; ++i) {
         const int64_t v0 = (int64_t)i * p.piece, here = std::min(p.piece, a.v - v0);
         s.v0 = (int)v0;
