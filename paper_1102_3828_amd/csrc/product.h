@@ -194,34 +194,34 @@ struct Product {
         const int wm = wave / WAVES_N * (BM / WAVES_M), wn = wave % WAVES_N * (BN / WAVES_N);
         const int r = lane & 15, g = lane >> 4;
         // where this lane's fragments of the first tile lie; the others at constant distances (the permutations repeat every 16 or 32 rows)
-        uint32_t pf[2], qf[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            // outer: the row of k (the column's chunk comes with the tile)
-            const int row = wm + 8 * (r >> 2) + 4 * j + (r & 3), k = 8 * g + 4 * j + (r >> 2);
-            pf[j] = P_OUTER ? k * (2 * BM) : row * ROW + 16 * (g ^ swz_p(row));
-            qf[j] = Q_OUTER ? k * (2 * BN) : (wn + r) * ROW + 16 * (g ^ swz_q(wn + r));
-        }
-        auto outer_read = [&](const char* b, const uint32_t (&rows)[2], int column, int swizzle) {   // eight k of column + (l & 15)
-            short8v v;
-            const int chunk = ((column >> 3) + ((r & 3) >> 1)) ^ swizzle;
+        uint32_t pf[2], qf[1];
+        {
+            const int k = 8 * g + (r >> 2), chunk = (r & 3) >> 1;   // outer: a row of k (and four further on), two lanes a chunk; tile t is 32 t bytes on, before the permutation
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const short4v h = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(b + rows[j] + 16 * chunk + 8 * (r & 1)));
+                const int row = wm + 8 * (r >> 2) + 4 * j + (r & 3);
+                pf[j] = P_OUTER ? k * (2 * BM) + 16 * (((wm >> 3) + chunk) ^ swz_k<BM>(k)) + 8 * (r & 1) : row * ROW + 16 * (g ^ swz_p(row));
+            }
+            qf[0] = Q_OUTER ? k * (2 * BN) + 16 * (((wn >> 3) + chunk) ^ swz_k<BN>(k)) + 8 * (r & 1) : (wn + r) * ROW + 16 * (g ^ swz_q(wn + r));
+        }
+        auto outer_read = [&](const char* stage, uint32_t first, int t, int size) {   // eight k of the tile's column l & 15
+            short8v v;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const short4v h = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(stage + (first ^ (32 * t)) + j * 8 * size));
                 v[4 * j] = h[0]; v[4 * j + 1] = h[1]; v[4 * j + 2] = h[2]; v[4 * j + 3] = h[3];
             }
             return v;
         };
-        const int pk = swz_k<BM>(8 * g + (r >> 2)), qk = swz_k<BN>(8 * g + (r >> 2));   // (the same four rows further on)
         // fragments of slice `sub` of a stage
         auto read_p = [&](const char* stage, int sub, int plane, int t) {
             const char* const b = stage + plane * P_BYTES;
-            if constexpr (P_OUTER) return outer_read(b + sub * (2 * BM * IVFR_PRODUCT_K), pf, wm + 16 * t, pk);
+            if constexpr (P_OUTER) return outer_read(b + sub * (2 * BM * IVFR_PRODUCT_K), pf[0], t, BM);
             else return *reinterpret_cast<const short8v*>(b + (pf[t & 1] ^ (64 * sub)) + (t >> 1) * 32 * ROW);
         };
         auto read_q = [&](const char* stage, int sub, int plane, int t) {
             const char* const b = stage + PLANES * P_BYTES + plane * Q_BYTES;
-            if constexpr (Q_OUTER) return outer_read(b + sub * (2 * BN * IVFR_PRODUCT_K), qf, wn + 16 * t, qk);
+            if constexpr (Q_OUTER) return outer_read(b + sub * (2 * BN * IVFR_PRODUCT_K), qf[0], t, BN);
             else return *reinterpret_cast<const short8v*>(b + (qf[0] ^ (64 * sub)) + t * 16 * ROW);
         };
         floatx4 acc[TM][TN];
