@@ -99,27 +99,27 @@ int product_join(const ProductOut& a, int a_slots, const ProductOut& b, int b_sl
     return IVFR_OK;
 }
 
-// Cycles of a slice on a compute unit that holds as many workgroups as it can, and that number, by what was measured; planes 1, 2, 3
+// What a product takes in each way, from what was measured: rounds of workgroups (as many at a time as the compute units hold), each so many us a
+// slice and a tile; partial sums are written and read again (at 3 TB/s), with a launch.  Planes 1 and 3.
 struct TileCost {
-    int resident[3];
-    double slice[3];
+    int resident[2];
+    double slice[2], tile;
 };
-static const TileCost COSTS[IVFR_TILES] = {{{1, 0, 0}, {1600, 0, 0}}, {{2, 1, 1}, {1000, 1500, 2600}},
-                                           {{2, 2, 2}, {320, 700, 1200}}, {{0, 0, 0}, {0, 0, 0}}, {{2, 0, 1}, {420, 0, 900}}};
+static const TileCost COSTS[IVFR_TILES] = {{{1, 0}, {0.95, 0}, 9}, {{2, 1}, {0.62, 1.3}, 6}, {{2, 2}, {0.30, 0.75}, 4}, {{0, 0}, {0, 0}, 0}, {{2, 1}, {0.17, 0.45}, 4}};
 
 void product_cut(int64_t np, int64_t nq, int64_t slices, int planes, bool q_outer, int* tile, int* splits) {
     double least = 1e300;
+    const int kind = planes == 1 ? 0 : 1;
     for (int k = 0; k < IVFR_TILES; ++k) {
-        const int resident = COSTS[k].resident[planes - 1];
+        const int resident = COSTS[k].resident[kind];
         if (!resident || (k == IVFR_TILE_128x16 && (q_outer || nq > 64))) continue;
         const int64_t tiles = ((np + IVFR_TILE_P[k] - 1) / IVFR_TILE_P[k]) * ((nq + IVFR_TILE_Q[k] - 1) / IVFR_TILE_Q[k]);
         for (int s = 1; s <= 128 && s <= slices; s *= 2) {
             const int64_t per = product_per((int)slices, s), parts = (slices + per - 1) / per, slots = (int64_t)IVFR_PRODUCT_CU * resident;
             const double rounds = (double)((tiles * parts + slots - 1) / slots);
-            // (workgroups that share a compute unit share its matrix units)
-            const double share = tiles * parts <= IVFR_PRODUCT_CU ? 0.6 : 1.0;
-            double cost = rounds * ((double)per * COSTS[k].slice[planes - 1] * share + 5000.0);
-            if (s > 1) cost += 6000.0 + (double)parts * np * nq * 8.0 / 1900.0;   // partial sums written and read, a launch
+            const double alone = resident > 1 && tiles * parts <= IVFR_PRODUCT_CU ? 0.75 : 1.0;   // a compute unit each
+            double cost = rounds * ((double)per * COSTS[k].slice[kind] * alone + COSTS[k].tile);
+            if (s > 1) cost += 6.0 + (double)parts * np * nq * 8.0 / 3.0e6;
             if (cost < least) {
                 least = cost;
                 *tile = k;
