@@ -354,14 +354,17 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, SMALL_WAVES / 4) void small_kerne
     m.g = (const char*)m.g + (int64_t)blockIdx.x * m.batch_stride * size;
     m.out = (char*)m.out + (int64_t)blockIdx.x * m.rows * m.cols * size;
     // the norm, then X, of values that are read once; columns of g past the end are zeros, rows are padded here
-    constexpr bool F32 = PLANES > 1;
-    constexpr int HELD = F32 && BLOCKS > 5 ? 5 : BLOCKS;   // pieces of eight that a thread has at most: 4096 values a block, and what LDS holds
+    constexpr int HELD = PLANES > 1 && BLOCKS > 5 ? 5 : BLOCKS;   // pieces of eight that a thread has at most: 4096 values a block, and what LDS holds
     const int chunks = (m.cols + 7) / 8, total = m.rows * chunks;
     float f[HELD][8];
 #pragma unroll
     for (int h = 0; h < HELD; ++h) {
         const int i = threadIdx.x + 64 * SMALL_WAVES * h, row = i / chunks, k = (i - row * chunks) * 8;
-        if (i < total) load_eight<F32>(m.g, (int64_t)row * m.ld + k, m.align, m.cols - k, m.type == IVFR_TYPE_F16, f[h]);
+        if (i >= total) continue;
+        const int64_t at = (int64_t)row * m.ld + k;
+        if constexpr (PLANES == 1) load_eight<false>(m.g, at, m.align, m.cols - k, false, f[h]);
+        else if (m.type == IVFR_TYPE_F32) load_eight<true>(m.g, at, m.align, m.cols - k, false, f[h]);   // uniform
+        else load_eight<false>(m.g, at, m.align, m.cols - k, true, f[h]);
     }
     for (int i = threadIdx.x; i < PLANES * xplane / 16; i += 64 * SMALL_WAVES) reinterpret_cast<uint4*>(X)[i] = make_uint4(0, 0, 0, 0);
     double s = 0.0;
@@ -534,11 +537,11 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, SMALL_WAVES / 4) void small_kerne
             if (four_at_once) {
                 const int64_t at = (int64_t)qrow * m.cols + col;
                 if (qrow >= m.rows || col >= m.cols) continue;
-                if constexpr (F32) *reinterpret_cast<floatx4*>((float*)m.out + at) = v;
+                if (PLANES > 1 && m.type == IVFR_TYPE_F32) *reinterpret_cast<floatx4*>((float*)m.out + at) = v;   // uniform
                 else {
                     short4v h;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) h[e] = (short)(m.type == IVFR_TYPE_F16 ? to_half(v[e]) : to_bf16(v[e]));
+                    for (int e = 0; e < 4; ++e) h[e] = (short)(PLANES > 1 ? to_half(v[e]) : to_bf16(v[e]));
                     *reinterpret_cast<short4v*>((uint16_t*)m.out + at) = h;
                 }
             } else {
@@ -600,7 +603,7 @@ static OrthoPlan ortho_plan(const ivfr_orthogonalize_args& a) {
     p.c = std::max(a.rows, a.cols);
     p.rp = (int)round_up(p.r, 32);
     p.cp = (int)round_up(p.c, 32);
-    p.planes = a.type == IVFR_TYPE_F32 ? 2 : 1;
+    p.planes = a.type == IVFR_TYPE_BF16 ? 1 : 2;
     p.batch = a.batch;
     p.xld = (int)product_ld(p.cp);
     p.ald = (int)product_ld(p.rp);

@@ -66,22 +66,22 @@ __device__ __forceinline__ bool product_work(uint32_t i, uint32_t block, uint32_
 inline unsigned product_grid(int64_t tiles, int resident) { return (unsigned)std::min<int64_t>((tiles + 7) / 8 * 8, (int64_t)IVFR_PRODUCT_CU * resident); }
 
 // PLANES of fp32 operands: 3 of bf16 (24 bits), of which the six products with a + b <= 2 are formed (what they neglect is 2^-24 of the whole), or 2 of
-// fp16 (22 bits and a sign), three products (2^-22).  All planes of a stage's k are in LDS at once.
-template <int BM_, int BN_, int WAVES_M_, int WAVES_N_, bool P_OUTER_, bool Q_OUTER_, bool HALF_, int PLANES_, int KSUB_, int STAGES_>
+// fp16 (22 bits and a sign), three products (2^-22).  All planes of a stage's k are in LDS at once.  Q_PLANES: of Q, where it has more.
+template <int BM_, int BN_, int WAVES_M_, int WAVES_N_, bool P_OUTER_, bool Q_OUTER_, bool HALF_, int PLANES_, int KSUB_, int STAGES_, int Q_PLANES_ = PLANES_>
 struct Product {
     static constexpr int BM = BM_, BN = BN_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_, WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES;
-    static constexpr int PLANES = PLANES_, KSUB = KSUB_, STAGES = STAGES_;      // slices of 32 k in a stage, LDS buffers
+    static constexpr int PLANES = PLANES_, Q_PLANES = Q_PLANES_, MOST = PLANES > Q_PLANES ? PLANES : Q_PLANES, KSUB = KSUB_, STAGES = STAGES_;      // slices of 32 k in a stage, LDS buffers
     static constexpr bool P_OUTER = P_OUTER_, Q_OUTER = Q_OUTER_, HALF = HALF_;
     static constexpr int TM = BM / WAVES_M / 16, TN = BN / WAVES_N / 16;
     // Inner operands lie in LDS as rows of a stage's k, outer ones as rows of their own index.  With KSUB 2 a row of an inner operand brings 128 bytes, a
     // whole line; with 64 the lines are fetched twice, by halves, and the L2 is what bounds the larger tiles.
     static constexpr int ROW = 2 * IVFR_PRODUCT_K * KSUB, CHUNKS = ROW / 16;    // bytes and 16-byte chunks of such a row
     static constexpr int P_BYTES = BM * ROW, Q_BYTES = BN * ROW;                // of a plane
-    static constexpr int STAGE = (P_BYTES + Q_BYTES) * PLANES, LDS = STAGES * STAGE;
+    static constexpr int STAGE = P_BYTES * PLANES + Q_BYTES * Q_PLANES, LDS = STAGES * STAGE;
     static constexpr int RESIDENT = 163840 / LDS >= 2 ? 2 : 1;                  // workgroups on a compute unit that registers are kept for
     static constexpr int WAVES_SIMD = WAVES * RESIDENT / 4 >= 1 ? WAVES * RESIDENT / 4 : 1;
     static constexpr int P_ROWS = P_BYTES / 1024, Q_ROWS = Q_BYTES / 1024;      // loads of 64 lanes x 16 bytes for one plane of a stage
-    static constexpr int P_LOADS = P_ROWS * PLANES, Q_LOADS = Q_ROWS * PLANES;
+    static constexpr int P_LOADS = P_ROWS * PLANES, Q_LOADS = Q_ROWS * Q_PLANES;
     // Every wavefront issues the same number of loads, so that one count of those in flight holds for all (what is left over is
     // issued twice, the same bytes to the same place).
     static constexpr int P_EACH = (P_LOADS + WAVES - 1) / WAVES, Q_EACH = (Q_LOADS + WAVES - 1) / WAVES, EACH = P_EACH + Q_EACH;
@@ -188,7 +188,7 @@ struct Product {
                 const int f = (wave + i * WAVES) % Q_LOADS, row = f % Q_ROWS, plane = f / Q_ROWS;
                 uint32_t o = qo[i % Q_KINDS];
                 if (q_part) o = source<Q_OUTER, BN, false>(row, lane, Q.ld, Q.extent - ahead.q * BN, q_left);
-                load16(base + PLANES * P_BYTES + plane * Q_BYTES + 1024 * row, o, qa + (PLANES > 1 ? plane * Q.plane : 0));
+                load16(base + PLANES * P_BYTES + plane * Q_BYTES + 1024 * row, o, qa + (Q_PLANES > 1 ? plane * Q.plane : 0));
             }
         };
         const int wm = wave / WAVES_N * (BM / WAVES_M), wn = wave % WAVES_N * (BN / WAVES_N);
@@ -226,7 +226,7 @@ struct Product {
         };
         floatx4 acc[TM][TN];
         ProductWork w;
-        constexpr int AHEAD = PLANES == 1 ? STAGES : STAGES - 1;   // stages loaded before the first one is used
+        constexpr int AHEAD = MOST == 1 ? STAGES : STAGES - 1;   // stages loaded before the first one is used
 #pragma unroll
         for (int s = 0; s < AHEAD; ++s) {
             prepare();
@@ -234,7 +234,7 @@ struct Product {
         }
         prepare();
         int buf = 0;   // of the stage that is being used
-        if constexpr (PLANES == 1) {
+        if constexpr (MOST == 1) {
             // The fragments of a slice are read during the products of the slice before, each of P in place of the one that has just been used.
             // Before the last slice of stage s all wavefronts have read all of s, so that its buffer is loaded with stage s + STAGES; the stages before that
             // are on their way, and s + 1 is needed.
@@ -316,23 +316,29 @@ struct Product {
                     for (int sub = 0; sub < KSUB; ++sub) {
                         if (KSUB > 1 && s + sub >= w.count) break;   // uniform
                         const char* const from = smem + buf * STAGE;
-                        short8v fp[PLANES][TM], fq[PLANES][TN];
+                        short8v fp[PLANES][TM], fq[Q_PLANES][TN];
 #pragma unroll
-                        for (int n = PLANES - 1; n >= 0; --n) {
+                        for (int n = MOST - 1; n >= 0; --n) {
+                            if (n < Q_PLANES) {
 #pragma unroll
-                            for (int t = 0; t < TN; ++t) fq[n][t] = read_q(from, sub, n, t);
+                                for (int t = 0; t < TN; ++t) fq[n][t] = read_q(from, sub, n, t);
+                            }
+                            if (n < PLANES) {
 #pragma unroll
-                            for (int t = 0; t < TM; ++t) fp[n][t] = read_p(from, sub, n, t);
+                                for (int t = 0; t < TM; ++t) fp[n][t] = read_p(from, sub, n, t);
+                            }
                         }
                         if (sub == 0) load(buf == 0 ? STAGES - 1 : buf - 1);   // (all have read the stage before)
 #pragma unroll
-                        for (int sum = PLANES - 1; sum >= 0; --sum)   // small products first
+                        for (int sum = MOST - 1; sum >= 0; --sum)   // small products first
 #pragma unroll
-                            for (int n = 0; n <= sum; ++n)
+                            for (int n = 0; n <= sum && n < PLANES; ++n) {
+                                if (sum - n >= Q_PLANES) continue;
 #pragma unroll
                                 for (int a = 0; a < TM; ++a)
 #pragma unroll
                                     for (int b = 0; b < TN; ++b) acc[a][b] = mfma(fp[n][a], fq[sum - n][b], acc[a][b]);
+                            }
                     }
                     prepare();
                     buf = buf + 1 == STAGES ? 0 : buf + 1;
@@ -362,6 +368,8 @@ struct Product {
     }
 };
 
+// planes: 1, 2 or 3 of both, or
+#define IVFR_PLANES_1_2 4   // one of P and two of Q
 // The tiles that there are.  256 x 256 reads least from LDS and memory per product and is the fastest wherever it gives every compute unit work (scores of 8192 x
 // 131072, d = 2048: 3.6 ms; in tiles of 256 x 128, two workgroups on a compute unit, 4.2; 128 x 128 5.0).  The smaller ones are for fewer outputs, the narrow ones for few rows.
 #define IVFR_TILE_256x256 0
@@ -379,6 +387,9 @@ template <bool PO, bool QO, bool HALF> struct ProductOf<3, PO, QO, HALF, 1> { ty
 template <bool PO, bool QO, bool HALF> struct ProductOf<4, PO, QO, HALF, 1> { typedef Product<128, 16, 4, 1, PO, QO, HALF, 1, 2, 4> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<1, PO, QO, HALF, 2> { typedef Product<128, 128, 2, 4, PO, QO, HALF, 2, 2, 2> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<2, PO, QO, HALF, 2> { typedef Product<64, 64, 2, 2, PO, QO, HALF, 2, 1, 4> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<1, PO, QO, HALF, 4> { typedef Product<128, 128, 2, 4, PO, QO, HALF, 1, 1, 3, 2> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<2, PO, QO, HALF, 4> { typedef Product<64, 64, 2, 2, PO, QO, HALF, 1, 1, 4, 2> T; };
+template <bool PO, bool QO, bool HALF> struct ProductOf<4, PO, QO, HALF, 4> { typedef Product<128, 16, 4, 1, PO, QO, HALF, 1, 2, 3, 2> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<1, PO, QO, HALF, 3> { typedef Product<128, 128, 2, 4, PO, QO, HALF, 3, 1, 3> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<2, PO, QO, HALF, 3> { typedef Product<64, 64, 2, 2, PO, QO, HALF, 3, 1, 3> T; };
 template <bool PO, bool QO, bool HALF> struct ProductOf<3, PO, QO, HALF, 3> { typedef Product<128, 64, 4, 1, PO, QO, HALF, 3, 1, 2> T; };

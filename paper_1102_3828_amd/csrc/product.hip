@@ -100,16 +100,16 @@ int product_join(const ProductOut& a, int a_slots, const ProductOut& b, int b_sl
 }
 
 // What a product takes in each way, from what was measured: rounds of workgroups (as many at a time as the compute units hold), each so many us a
-// slice and a tile; partial sums are written and read again (at 3 TB/s), with a launch.  Planes 1 and 3.
+// slice and a tile; partial sums are written and read again (at 3 TB/s), with a launch.  Planes 1, 3, 1 and 2.
 struct TileCost {
-    int resident[2];
-    double slice[2], tile;
+    int resident[3];
+    double slice[3], tile;
 };
-static const TileCost COSTS[IVFR_TILES] = {{{1, 0}, {0.95, 0}, 9}, {{2, 1}, {0.62, 1.3}, 6}, {{2, 2}, {0.30, 0.75}, 4}, {{0, 0}, {0, 0}, 0}, {{2, 1}, {0.17, 0.45}, 4}};
+static const TileCost COSTS[IVFR_TILES] = {{{1, 0, 0}, {0.95, 0, 0}, 9}, {{2, 1, 2}, {0.62, 1.3, 1.0}, 6}, {{2, 2, 2}, {0.30, 0.75, 0.40}, 4}, {{0, 0, 0}, {0, 0, 0}, 0}, {{2, 1, 2}, {0.17, 0.45, 0.2}, 4}};
 
 void product_cut(int64_t np, int64_t nq, int64_t slices, int planes, bool q_outer, int* tile, int* splits) {
     double least = 1e300;
-    const int kind = planes == 1 ? 0 : 1;
+    const int kind = planes == 1 ? 0 : planes == 3 ? 1 : 2;
     for (int k = 0; k < IVFR_TILES; ++k) {
         const int resident = COSTS[k].resident[kind];
         if (!resident || (k == IVFR_TILE_128x16 && (q_outer || nq > 64))) continue;
@@ -175,5 +175,6 @@ static int launch_both(const ProductOut& x, const ProductOut& w, hipStream_t st)
 
 int product_launch(const ProductOut& x, const ProductOut& w, bool half, hipStream_t st) {
     if (x.planes == 3) return launch_both<false, 3>(x, w, st);
+    if (x.planes == IVFR_PLANES_1_2) return half ? launch_both<true, IVFR_PLANES_1_2>(x, w, st) : launch_both<false, IVFR_PLANES_1_2>(x, w, st);
     return half ? launch_both<true, 1>(x, w, st) : launch_both<false, 1>(x, w, st);
 }

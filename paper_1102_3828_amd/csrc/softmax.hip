@@ -125,7 +125,9 @@ struct ScoreArgs {
     float* target_score;       // [n]
     // gradient
     const float* lse;          // [n]
+    const float2* stat;        // [n] of fp32 calls, in its place (see loss_kernel)
     const float* weight;       // [n]
+    int e_planes;              // 16-bit values per e
     const float* unit;         // unit[0] is a factor of e, or null
     uint16_t* e;               // [planes][panels of 256 vectors][n_pad][256]
     int64_t e_plane;           // elements of a plane
@@ -236,9 +238,12 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void score_kernel(ScoreA
            });
 }
 
-// A wavefront per row joins its tiles' statistics (in a fixed order).
+// A wavefront per row joins its tiles' statistics (in a fixed order).  stat: of the gradients of fp32 calls, (maximum, log2 of the sum) in the unit of the
+// scores.  One fp32 number for both would make p - 1 of a target that has nearly all of the probability wrong by ten times what the products make it.  Where the
+// caller gives a logarithm of his own (of a larger set, say), that stands; where it is this one, rounded, the two parts do.
 __global__ __launch_bounds__(256) void loss_kernel(const float2* __restrict__ part, int tiles, const float* __restrict__ target_score,
-                                                   const int64_t* __restrict__ targets, int n, int64_t v, float* __restrict__ loss, float* __restrict__ lse) {
+                                                   const int64_t* __restrict__ targets, int n, int64_t v, float* __restrict__ loss, float* __restrict__ lse,
+                                                   const float* __restrict__ given, float2* __restrict__ stat) {
     const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (i >= n) return;   // uniform over a wavefront
     const float2* p = part + (int64_t)i * tiles;
@@ -266,6 +271,11 @@ __global__ __launch_bounds__(256) void loss_kernel(const float2* __restrict__ pa
     if (lane == 0) {
         const float ls = log2f(s), L = m == -INFINITY && s == 0.f ? -INFINITY : (m + ls) * LN2;
         if (lse) lse[i] = L;
+        if (stat) {
+            float2 two = L == -INFINITY ? make_float2(0.f, 0.f) : make_float2(m, ls);   // nothing takes part: powers of -inf, not NaN
+            if (given && given[i] != L) two = make_float2(given[i] == -INFINITY ? 0.f : given[i] * LOG2E, 0.f);
+            stat[i] = two;
+        }
         if (loss) {
             const int64_t t = targets[i];
             float x;
@@ -291,18 +301,23 @@ __device__ __forceinline__ void write_factors(const ScoreArgs& a, const ProductW
         const int i = q0 + C::q_of(tid, u);
         if (i >= a.n_pad) continue;
         int64_t target = -1;
-        float L = 0.f, g = 0.f;
+        float top = 0.f, ls = 0.f, g = 0.f;
         if (i < a.n) {
             target = a.targets[i];
-            L = a.lse[i];
-            if (L == -INFINITY) L = 0.f;   // nothing takes part: powers of -inf, not NaN
+            if constexpr (C::PLANES > 1) {
+                top = a.stat[i].x;
+                ls = a.stat[i].y;
+            } else {
+                top = a.lse[i];
+                top = top == -INFINITY ? 0.f : top * LOG2E;   // nothing takes part: powers of -inf, not NaN
+            }
             g = target < 0 ? 0.f : a.weight[i] * unit;
             if (target >= a.v_all && g != 0.f) g = NAN;
         }
 #pragma unroll
         for (int t = 0; t < C::TM; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) acc[t][u][r] = __builtin_amdgcn_exp2f(fmaf(L, -LOG2E, acc[t][u][r]));
+            for (int r = 0; r < 4; ++r) acc[t][u][r] = __builtin_amdgcn_exp2f(C::PLANES == 1 ? acc[t][u][r] - top : (acc[t][u][r] - top) - ls);
         {   // the row's own vector, if it is in this tile and takes part: p - 1 before anything is rounded
             int at = target >= (int64_t)a.v0 + p0 && target < (int64_t)a.v0 + a.v && target < (int64_t)a.v0 + p0 + C::BM ? (int)(target - a.v0 - p0) : -1;
             if (at >= 0 && a.offset && a.offset[p0 + at] == -INFINITY) at = -1;
@@ -324,22 +339,21 @@ __device__ __forceinline__ void write_factors(const ScoreArgs& a, const ProductW
             for (int r = 0; r < 8; ++r) f[r] = g * acc[t + (r >> 2)][u][r & 3];
             uint16_t* const o = a.e + ((int64_t)(j >> 8) * a.n_pad + i) * 256 + (j & 255);
 #pragma unroll
-            for (int p = 0; p < C::PLANES; ++p) {
+            for (int p = 0; p < (C::PLANES == 1 && C::BM < 256 ? 2 : C::PLANES); ++p) {   // (the largest tile has no registers for a second)
+                if (C::PLANES == 1 && p > 0 && a.e_planes < 2) break;   // uniform
                 short8v h;
 #pragma unroll
                 for (int r = 0; r < 8; ++r) {
-                    if constexpr (C::HALF) h[r] = (short)to_half(f[r]);
-                    else {
-                        const uint16_t b = to_bf16(f[r]);
-                        h[r] = (short)b;
-                        if constexpr (C::PLANES > 1) f[r] -= from_bf16(b);
-                    }
+                    const uint16_t b = C::HALF ? to_half(f[r]) : to_bf16(f[r]);
+                    h[r] = (short)b;
+                    f[r] -= C::HALF ? from_half(b) : from_bf16(b);
                 }
                 if (!live) h = short8v{0, 0, 0, 0, 0, 0, 0, 0};
                 *reinterpret_cast<short8v*>(o + p * a.e_plane) = h;
             }
         }
-    }}
+    }
+}
 
 template <class C>
 __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void grad_score_kernel(ScoreArgs a) {
@@ -402,7 +416,8 @@ struct SoftmaxPlan {
     int pieces;
     int64_t tiles_p;                  // of the loss
     int dx_tile, dx_splits, dw_tile, dw_splits;   // of a whole piece
-    int64_t at_x, at_w, at_part, at_target, at_lse, at_unit, at_e, at_dx, at_dw, bytes;
+    int64_t at_x, at_w, at_part, at_target, at_stat, at_unit, at_e, at_dx, at_dw, bytes;
+    int e_planes, planes_of_out;
 };
 
 static bool rows_aligned(const void* p, int64_t ld, int size) { return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0; }
@@ -444,17 +459,21 @@ static SoftmaxPlan softmax_plan(const ivfr_softmax_args& a, bool grad) {
     p.at_part = take(a.n * p.tiles_p * 8);
     p.at_target = take(a.n * 4);
     if (grad) {
-        p.at_lse = take(a.n * 4);
+        p.at_stat = take(a.n * 8);
+        // Two 16-bit values of each e where there are few rows: there the rounding of single large ones shows in the gradients (up to 3.6 times the error of a
+        // gradient that is rounded once, to its own type), and the products are not what such a call waits for.  Of many rows one value is enough: 1.4 times.
+        p.e_planes = f32 ? 3 : a.n <= 512 ? 2 : 1;
+        p.planes_of_out = f32 ? 3 : p.e_planes == 2 ? IVFR_PLANES_1_2 : 1;
         p.at_unit = take(8);
         // pieces of equal width, a multiple of 256
-        const int64_t fit = std::max<int64_t>(256, GRAD_PIECE_BYTES / (2 * p.planes * p.n_pad) / 256 * 256);
+        const int64_t fit = std::max<int64_t>(256, GRAD_PIECE_BYTES / (2 * p.e_planes * p.n_pad) / 256 * 256);
         p.pieces = (int)((a.v + fit - 1) / fit);
         p.piece = std::min(round_up((a.v + p.pieces - 1) / p.pieces, 256), round_up(a.v, 32));
         p.pieces = (int)((a.v + p.piece - 1) / p.piece);
         p.e_plane = (p.piece + 255) / 256 * p.n_pad * 256;
-        p.at_e = take(p.planes * p.e_plane * 2);
-        product_cut(a.d, a.n, (p.piece + 31) / 32, p.planes, false, &p.dx_tile, &p.dx_splits);
-        product_cut(a.d, p.piece, p.n_pad / 32, p.planes, true, &p.dw_tile, &p.dw_splits);
+        p.at_e = take(p.e_planes * p.e_plane * 2);
+        product_cut(a.d, a.n, (p.piece + 31) / 32, p.planes_of_out, false, &p.dx_tile, &p.dx_splits);
+        product_cut(a.d, p.piece, p.n_pad / 32, p.planes_of_out, true, &p.dw_tile, &p.dw_splits);
         if (p.pieces > 1 || p.dx_splits > 1) p.at_dx = take((int64_t)p.pieces * p.dx_splits * a.n * product_pad(a.d) * 4);
         if (p.dw_splits > 1) p.at_dw = take(p.dw_splits * p.piece * product_pad(a.d) * 4);
     }
@@ -520,9 +539,9 @@ static int prepare(const ivfr_softmax_args& a, const SoftmaxPlan& p, const float
     return IVFR_OK;
 }
 
-static int statistics(const ivfr_softmax_args& a, const SoftmaxPlan& p, ScoreArgs s, float* loss, float* lse, hipStream_t st) {
+static int statistics(const ivfr_softmax_args& a, const SoftmaxPlan& p, ScoreArgs s, float* loss, float* lse, const float* given, float2* stat, hipStream_t st) {
     IVFR_TRY(launch_scores(s, p.tile, p.half, false, st));
-    hipLaunchKernelGGL(loss_kernel, dim3((unsigned)((a.n + 3) / 4)), dim3(256), 0, st, s.part, (int)p.tiles_p, s.target_score, a.targets, (int)a.n, a.v, loss, lse);
+    hipLaunchKernelGGL(loss_kernel, dim3((unsigned)((a.n + 3) / 4)), dim3(256), 0, st, s.part, (int)p.tiles_p, s.target_score, a.targets, (int)a.n, a.v, loss, lse, given, stat);
     IVFR_HIP(hipGetLastError());
     return IVFR_OK;
 }
@@ -537,7 +556,7 @@ int ivfr_softmax_loss(const ivfr_softmax_args* args, float* loss, float* lse, vo
     hipStream_t st = (hipStream_t)stream;
     ScoreArgs s = {};
     IVFR_TRY(prepare(*args, p, nullptr, (char*)workspace, s, st));
-    return statistics(*args, p, s, loss, lse, st);
+    return statistics(*args, p, s, loss, lse, nullptr, nullptr, st);
 }
 
 __global__ __launch_bounds__(256) void zero_kernel(uint4* p, int64_t chunks, uint8_t* tail, int rest) {
@@ -567,12 +586,16 @@ int ivfr_softmax_loss_grad(const ivfr_softmax_args* args, const float* weight, c
     char* const ws = (char*)workspace;
     ScoreArgs s = {};
     IVFR_TRY(prepare(a, p, weight, ws, s, st));
-    if (!lse || loss) {
-        float* const own_lse = (float*)(ws + p.at_lse);
-        IVFR_TRY(statistics(a, p, s, loss, own_lse, st));
-        if (!lse) lse = own_lse;
+    if (p.planes > 1) {   // (with the caller's lse too)
+        s.stat = (float2*)(ws + p.at_stat);
+        IVFR_TRY(statistics(a, p, s, loss, nullptr, lse, (float2*)(ws + p.at_stat), st));
+    } else if (!lse || loss) {
+        float* const own = (float*)(ws + p.at_stat);
+        IVFR_TRY(statistics(a, p, s, loss, own, nullptr, nullptr, st));
+        if (!lse) lse = own;
     }
     s.lse = lse;
+    s.e_planes = p.e_planes;
     s.e = (uint16_t*)(ws + p.at_e);
     s.e_plane = p.e_plane;
     s.n_pad = (int)p.n_pad;
@@ -591,8 +614,9 @@ int ivfr_softmax_loss_grad(const ivfr_softmax_args* args, const float* weight, c
         s.w.base = w.base + v0 * w.ld;
         s.w.extent = (int)here;
         s.offset = a.offset ? a.offset + v0 : nullptr;
-        IVFR_TRY(launch_scores(s, score_tile(a.n, here, p.planes), p.half, true, st));
-        ox.planes = s.planes;
+        const int tile = score_tile(a.n, here, p.planes);
+        IVFR_TRY(launch_scores(s, p.e_planes == 2 && tile == IVFR_TILE_256x256 ? IVFR_TILE_128x128 : tile, p.half, true, st));
+        ox.planes = p.planes_of_out;
         ox.type = a.type;
         ox.alpha = a.scale;
         ox.unit = s.unit;
