@@ -7,8 +7,10 @@
 //
 // Every number of X, A and B is bounded by the singular values (which the coefficients keep in range, checked by the host), so the products run in
 // fp16 at a fixed scale of 2^12: three more bits than bf16 at the same rate, and values down to 2^-26 of the largest keep them all.
-// fp32 matrices are carried by two fp16 planes (22 bits and a sign), three products.  A and A^2 are symmetric: the tiles on and below the
-// diagonal are formed and written twice.  Sums are fp32; X, A and B are rounded once per product, to the planes that the next one reads.
+// Two planes of fp16 (22 bits and a sign), three products: errors of 5e-7 to 2e-6 of the result.  One plane, one product, for bf16 matrices with more than 128
+// on their shorter side: 1e-3 to 1.5e-3, less than the rounding of the result to bf16 (1.7e-3); with few singular values it would be up to 3e-3.
+// A and A^2 are symmetric: the tiles on and below the diagonal are formed and written twice.  Sums are fp32; X, A and B are rounded once per product, to the
+// planes that the next one reads.
 // All sides are padded with zeros to whole stages of 32.
 #include "product.h"
 
@@ -315,7 +317,7 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void update_kernel(StepA
 #define SMALL_LDS_HALF 81664   // two workgroups on a compute unit
 
 inline int small_blocks(int rp, int cp) { return (cp / 32 + SMALL_WAVES / (rp / 16) - 1) / (SMALL_WAVES / (rp / 16)); }   // of a wavefront
-inline int64_t small_lds(int rp, int cp, int planes) { return (int64_t)planes * rp * (cp + rp) * 2; }
+inline int64_t small_lds(int rp, int cp) { return (int64_t)2 * rp * (cp + rp) * 2; }
 
 struct SmallArgs {
     MatrixArgs m;
@@ -325,24 +327,22 @@ struct SmallArgs {
 struct Inner { static constexpr bool value = false; };   // how an operand lies
 struct Outer { static constexpr bool value = true; };
 
-// N values into their planes; two planes: the first one truncated (the second has what is left, to the nearest)
-template <int PLANES, int N>
-__device__ __forceinline__ void split_planes(const float (&v)[N], uint32_t (&h)[PLANES][N / 2]) {
+// N values into two planes: the first one truncated, the second has what is left, to the nearest
+template <int N>
+__device__ __forceinline__ void split_planes(const float (&v)[N], uint32_t (&h)[2][N / 2]) {
 #pragma unroll
     for (int e = 0; e < N; e += 2) {
-        if constexpr (PLANES == 1) h[0][e / 2] = to_half(v[e]) | (uint32_t)to_half(v[e + 1]) << 16;
-        else {
-            const auto top = __builtin_amdgcn_cvt_pkrtz(v[e], v[e + 1]);
-            h[0][e / 2] = __builtin_bit_cast(uint32_t, top);
-            h[1][e / 2] = to_half(fmaf((float)top[0], -1.f, v[e])) | (uint32_t)to_half(fmaf((float)top[1], -1.f, v[e + 1])) << 16;
-        }
+        const auto top = __builtin_amdgcn_cvt_pkrtz(v[e], v[e + 1]);
+        h[0][e / 2] = __builtin_bit_cast(uint32_t, top);
+        h[1][e / 2] = to_half(fmaf((float)top[0], -1.f, v[e])) | (uint32_t)to_half(fmaf((float)top[1], -1.f, v[e + 1])) << 16;
     }
 }
 
-template <int PLANES, int BLOCKS, int LDS>
+template <int BLOCKS, int LDS>
 __global__ __launch_bounds__(64 * SMALL_WAVES, SMALL_WAVES / 4) void small_kernel(const SmallArgs a) {
     __shared__ __align__(16) char smem[LDS];
     __shared__ double red[SMALL_WAVES];
+    constexpr int PLANES = 2;
     MatrixArgs m = a.m;
     const int rp = m.rp, cp = m.cp, slice = rp * 64, xplane = slice * (cp / 32), aplane = slice * (rp / 32);   // bytes
     char* const X = smem;
@@ -354,7 +354,7 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, SMALL_WAVES / 4) void small_kerne
     m.g = (const char*)m.g + (int64_t)blockIdx.x * m.batch_stride * size;
     m.out = (char*)m.out + (int64_t)blockIdx.x * m.rows * m.cols * size;
     // the norm, then X, of values that are read once; columns of g past the end are zeros, rows are padded here
-    constexpr int HELD = PLANES > 1 && BLOCKS > 5 ? 5 : BLOCKS;   // pieces of eight that a thread has at most: 4096 values a block, and what LDS holds
+    constexpr int HELD = BLOCKS > 5 ? 5 : BLOCKS;   // pieces of eight that a thread has at most: 4096 values a block, and what LDS holds
     const int chunks = (m.cols + 7) / 8, total = m.rows * chunks;
     float f[HELD][8];
 #pragma unroll
@@ -362,9 +362,8 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, SMALL_WAVES / 4) void small_kerne
         const int i = threadIdx.x + 64 * SMALL_WAVES * h, row = i / chunks, k = (i - row * chunks) * 8;
         if (i >= total) continue;
         const int64_t at = (int64_t)row * m.ld + k;
-        if constexpr (PLANES == 1) load_eight<false>(m.g, at, m.align, m.cols - k, false, f[h]);
-        else if (m.type == IVFR_TYPE_F32) load_eight<true>(m.g, at, m.align, m.cols - k, false, f[h]);   // uniform
-        else load_eight<false>(m.g, at, m.align, m.cols - k, true, f[h]);
+        if (m.type == IVFR_TYPE_F32) load_eight<true>(m.g, at, m.align, m.cols - k, false, f[h]);   // uniform
+        else load_eight<false>(m.g, at, m.align, m.cols - k, m.type == IVFR_TYPE_F16, f[h]);
     }
     for (int i = threadIdx.x; i < PLANES * xplane / 16; i += 64 * SMALL_WAVES) reinterpret_cast<uint4*>(X)[i] = make_uint4(0, 0, 0, 0);
     double s = 0.0;
@@ -389,7 +388,7 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, SMALL_WAVES / 4) void small_kerne
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[h][e] = (float)(f[h][e] * inv);
         uint32_t b[PLANES][4];
-        split_planes<PLANES>(f[h], b);
+        split_planes(f[h], b);
 #pragma unroll
         for (int n = 0; n < PLANES; ++n) {
             if (m.tall) {
@@ -455,7 +454,7 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, SMALL_WAVES / 4) void small_kerne
     auto put_a = [&](int i, const floatx4 (&o)[2]) {
         float v[8] = {o[0][0], o[0][1], o[0][2], o[0][3], o[1][0], o[1][1], o[1][2], o[1][3]};
         uint32_t h[PLANES][4];
-        split_planes<PLANES>(v, h);
+        split_planes(v, h);
 #pragma unroll
         for (int z = 0; z < PLANES; ++z) *reinterpret_cast<uint4*>(A + z * aplane + aplace + i * share * slice) = make_uint4(h[z][0], h[z][1], h[z][2], h[z][3]);
     };
@@ -519,7 +518,7 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, SMALL_WAVES / 4) void small_kerne
             for (int t = 0; t < 2; ++t) {
                 const float v[4] = {out[i][t][0], out[i][t][1], out[i][t][2], out[i][t][3]};
                 uint32_t h[PLANES][2];
-                split_planes<PLANES>(v, h);
+                split_planes(v, h);
 #pragma unroll
                 for (int z = 0; z < PLANES; ++z) *reinterpret_cast<uint2*>(X + z * xplane + (xplace ^ (32 * t)) + i * share * slice) = make_uint2(h[z][0], h[z][1]);
             }
@@ -537,11 +536,11 @@ __global__ __launch_bounds__(64 * SMALL_WAVES, SMALL_WAVES / 4) void small_kerne
             if (four_at_once) {
                 const int64_t at = (int64_t)qrow * m.cols + col;
                 if (qrow >= m.rows || col >= m.cols) continue;
-                if (PLANES > 1 && m.type == IVFR_TYPE_F32) *reinterpret_cast<floatx4*>((float*)m.out + at) = v;   // uniform
+                if (m.type == IVFR_TYPE_F32) *reinterpret_cast<floatx4*>((float*)m.out + at) = v;   // uniform
                 else {
                     short4v h;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) h[e] = (short)(PLANES > 1 ? to_half(v[e]) : to_bf16(v[e]));
+                    for (int e = 0; e < 4; ++e) h[e] = (short)(m.type == IVFR_TYPE_F16 ? to_half(v[e]) : to_bf16(v[e]));
                     *reinterpret_cast<short4v*>((uint16_t*)m.out + at) = h;
                 }
             } else {
@@ -603,7 +602,8 @@ static OrthoPlan ortho_plan(const ivfr_orthogonalize_args& a) {
     p.c = std::max(a.rows, a.cols);
     p.rp = (int)round_up(p.r, 32);
     p.cp = (int)round_up(p.c, 32);
-    p.planes = a.type == IVFR_TYPE_BF16 ? 1 : 2;
+    // one plane is as good as bf16 results where there are many singular values, whose errors then do not add up in one direction
+    p.planes = a.type == IVFR_TYPE_BF16 && p.rp > 128 ? 1 : 2;
     p.batch = a.batch;
     p.xld = (int)product_ld(p.cp);
     p.ald = (int)product_ld(p.rp);
@@ -615,8 +615,8 @@ static OrthoPlan ortho_plan(const ivfr_orthogonalize_args& a) {
         at += round_up(bytes, 256);
         return here;
     };
-    // (whatever fits: 128 x 128 in fp32 44 us against 91 in launches, 128 x 448 in bf16 88 against 88, 32 x 32 10 against 70)
-    p.small = small_lds(p.rp, p.cp, p.planes) <= SMALL_LDS && p.rp <= 128 && small_blocks(p.rp, p.cp) <= SMALL_BLOCKS;
+    // (whatever fits: 128 x 128 44 us against 90 in launches, 64 x 500 44 against 98, 32 x 32 10 against 71)
+    p.small = small_lds(p.rp, p.cp) <= SMALL_LDS && p.rp <= 128 && small_blocks(p.rp, p.cp) <= SMALL_BLOCKS;
     if (p.small) return p;
     p.parts = (int)std::min<int64_t>(ORTHO_SUMS, (p.xsize + 8191) / 8192);
     p.at_sums = take(p.batch * p.parts * 8);
@@ -709,20 +709,13 @@ static int launch_small(const MatrixArgs& m, const ivfr_orthogonalize_args& a, h
     for (int i = 0; i < a.steps; ++i)
         for (int j = 0; j < 3; ++j) s.k[i][j] = a.coefficients[3 * i + j];
     const dim3 grid((unsigned)a.batch);
-    const bool half = small_lds(m.rp, m.cp, m.planes) <= SMALL_LDS_HALF;
+    const bool half = small_lds(m.rp, m.cp) <= SMALL_LDS_HALF;
     const int blocks = small_blocks(m.rp, m.cp);
-#define IVFR_SMALL(PLANES, BLOCKS, LDS) hipLaunchKernelGGL((small_kernel<PLANES, BLOCKS, LDS>), grid, dim3(64 * SMALL_WAVES), 0, st, s)
-    if (m.planes == 1) {
-        if (blocks <= 2) IVFR_SMALL(1, 2, SMALL_LDS_HALF);   // (at most 128 x 128)
-        else if (blocks <= 4 && half) IVFR_SMALL(1, 4, SMALL_LDS_HALF);
-        else if (blocks <= 4) IVFR_SMALL(1, 4, SMALL_LDS);
-        else IVFR_SMALL(1, SMALL_BLOCKS, SMALL_LDS);
-    } else {
-        if (blocks <= 2 && half) IVFR_SMALL(2, 2, SMALL_LDS_HALF);
-        else if (blocks <= 2) IVFR_SMALL(2, 2, SMALL_LDS);
-        else if (blocks <= 4) IVFR_SMALL(2, 4, SMALL_LDS);
-        else IVFR_SMALL(2, SMALL_BLOCKS, SMALL_LDS);
-    }
+#define IVFR_SMALL(BLOCKS, LDS) hipLaunchKernelGGL((small_kernel<BLOCKS, LDS>), grid, dim3(64 * SMALL_WAVES), 0, st, s)
+    if (blocks <= 2 && half) IVFR_SMALL(2, SMALL_LDS_HALF);
+    else if (blocks <= 2) IVFR_SMALL(2, SMALL_LDS);
+    else if (blocks <= 4) IVFR_SMALL(4, SMALL_LDS);
+    else IVFR_SMALL(SMALL_BLOCKS, SMALL_LDS);
 #undef IVFR_SMALL
     IVFR_HIP(hipGetLastError());
     return IVFR_OK;
