@@ -277,8 +277,9 @@ int ivfr_stage_times(const ivfr_index* index, double* ms, int32_t* scan_launches
  * the loss +INFINITY.  A row with every vector left out has lse -INFINITY and no gradient.  Other components must be finite,
  * else losses and gradients that they enter are not numbers.
  * ivfr_softmax_loss: loss, lse fp32 [n].
- * ivfr_softmax_loss_grad: weight fp32 [n], the gradient of each row's loss; lse fp32 [n] of ivfr_softmax_loss for these arguments, or NULL
- * (it is then formed here); loss fp32 [n], or NULL; dx [n, d] and dw [v, d] dense, of the inputs' type, aligned to 16 bytes.
+ * ivfr_softmax_loss_grad: weight fp32 [n], the gradient of each row's loss; lse fp32 [n] of ivfr_softmax_loss for these arguments (or of a larger
+ * set), or NULL: it is then formed here, as in fp32 calls always (a number of 24 bits says too little of a target with nearly all of the probability).
+ * e is rounded to the inputs' type where it enters the products of bf16 and fp16 calls with more than 512 rows, to twice its bits with fewer; loss fp32 [n], or NULL; dx [n, d] and dw [v, d] dense, of the inputs' type, aligned to 16 bytes.
  * fp16 gradients below 2^-24 are zero in that type: scale the weights as for any training in fp16.  The order of every sum is fixed:
  * the same call gives the same bits. */
 typedef struct {
@@ -304,8 +305,8 @@ int ivfr_softmax_loss_grad(const ivfr_softmax_args* args, const float* weight, c
  * (with the shorter side as the rows of X).  out is close to the nearest matrix of orthonormal rows or columns: singular vectors stay, a
  * singular value s becomes a s + b s^3 + c s^5 in each step.  coefficients: host fp32 [steps][3] of (a, b, c); refused
  * (IVFR_ERR_INVALID_ARG) when singular values of up to 1 would leave (-15, 15) under them.  (3.4445, -4.7750, 2.0315), five times,
- * takes values from 0.01 to 1 into 0.7 to 1.2.  The products of bf16 and fp16 matrices are formed in fp16 at a fixed scale, with 11 bits
- * of every number of X, A and B; those of fp32 matrices with 22 bits.  A matrix of zeros stays zero (eps > 0); what is not finite makes its
+ * takes values from 0.01 to 1 into 0.7 to 1.2.  The products are formed in fp16 at a fixed scale, with 22 bits of every number of X, A and
+ * B; of bf16 matrices with more than 128 rows and columns with 11 bits.  A matrix of zeros stays zero (eps > 0); what is not finite makes its
  * matrix NaN.  out: dense [batch][rows, cols], of the type of g.  The order of every sum is fixed. */
 typedef struct {
     int64_t batch;               /* at most 65535                                            */

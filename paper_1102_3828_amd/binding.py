@@ -352,7 +352,7 @@ def softmax_loss(x, w, targets, scale=1.0, offset=None, stream=None):
 
 def softmax_loss_grad(x, w, targets, weight, scale=1.0, offset=None, lse=None, stream=None):
     """The gradients of sum_i weight_i loss_i.  weight: float32 [n].  Returns (loss, dx, dw), dx and dw of the inputs' type; with lse
-    (of softmax_loss for the same arguments) given, the statistics are not formed again and loss is None."""
+    (of softmax_loss for the same arguments) given, loss is None, and float16 and bfloat16 calls do not form the statistics again."""
     device = x.device
     handle, context = _on(stream, device)
     with context:

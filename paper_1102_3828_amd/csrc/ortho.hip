@@ -564,7 +564,7 @@ static int ortho_check(const ivfr_orthogonalize_args* a) {
     IVFR_REQUIRE(a->batch >= 0 && a->batch <= 65535 && a->rows >= 1 && a->cols >= 1 && a->rows <= 1 << 20 && a->cols <= 1 << 20,
                  "orthogonalize: batch must be in [0, 65535], rows and cols in [1, 2^20], got %lld, %d, %d", (long long)a->batch, a->rows, a->cols);
     IVFR_REQUIRE(std::min(a->rows, a->cols) <= 1 << 16, "orthogonalize: the shorter side must be at most 65536, got %d", std::min(a->rows, a->cols));
-    IVFR_REQUIRE(a->ld >= a->cols && a->batch_stride >= 0 && (a->batch <= 1 || a->batch_stride >= (a->rows - 1) * a->ld + a->cols), "orthogonalize: ld must be at least cols, and matrices must not overlap");
+    IVFR_REQUIRE(a->ld >= a->cols && a->ld <= 1ll << 40 && a->batch_stride >= 0 && (a->batch <= 1 || a->batch_stride >= (a->rows - 1) * a->ld + a->cols), "orthogonalize: ld must be at least cols, and matrices must not overlap");
     IVFR_REQUIRE(a->steps >= 1 && a->steps <= 64 && a->coefficients, "orthogonalize: 1 to 64 steps with coefficients, got %d", a->steps);
     IVFR_REQUIRE(std::isfinite(a->scale) && a->eps >= 0.f && std::isfinite(a->eps), "orthogonalize: scale must be finite, eps finite and not negative");
     // what a singular value, at most 1 at first, can become; the numbers of X, A and B are held in fp16 at 2^12, up to 16
