@@ -420,7 +420,7 @@ struct ProductOut {            // out[q][p] = alpha * unit * sum_k P(p, k) Q(q, 
     int tile, splits;          // how it is cut (product_cut)
 };
 // The tile and the number of parts of k for a product of these sizes; q_outer: Q too.
-void product_cut(int64_t np, int64_t nq, int64_t slices, int planes, bool q_outer, int* tile, int* splits);
+void product_cut(int64_t np, int64_t nq_x, int64_t slices_x, int64_t nq_w, int64_t slices_w, int planes, int* tile_x, int* splits_x, int* tile_w, int* splits_w);
 // slices of a part: whole stages
 __host__ __device__ inline int product_per(int slices, int splits) { return ((slices + splits - 1) / splits + 1) / 2 * 2; }
 inline int64_t product_pad(int64_t np) { return (np + 3) / 4 * 4; }

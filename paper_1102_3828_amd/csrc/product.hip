@@ -107,25 +107,42 @@ struct TileCost {
 };
 static const TileCost COSTS[IVFR_TILES] = {{{1, 0, 0}, {0.95, 0, 0}, 9}, {{2, 1, 2}, {0.62, 1.3, 1.0}, 6}, {{2, 2, 2}, {0.30, 0.75, 0.40}, 4}, {{0, 0, 0}, {0, 0, 0}, 0}, {{2, 1, 2}, {0.17, 0.45, 0.2}, 4}};
 
-void product_cut(int64_t np, int64_t nq, int64_t slices, int planes, bool q_outer, int* tile, int* splits) {
+// the splits that take least with one tile, and what they take
+static double cut_with(int k, int64_t np, int64_t nq, int64_t slices, int planes, bool q_outer, int* splits) {
     double least = 1e300;
-    const int kind = planes == 1 ? 0 : planes == 3 ? 1 : 2;
-    for (int k = 0; k < IVFR_TILES; ++k) {
-        const int resident = COSTS[k].resident[kind];
-        if (!resident || (k == IVFR_TILE_128x16 && (q_outer || nq > 64))) continue;
-        const int64_t tiles = ((np + IVFR_TILE_P[k] - 1) / IVFR_TILE_P[k]) * ((nq + IVFR_TILE_Q[k] - 1) / IVFR_TILE_Q[k]);
-        for (int s = 1; s <= 128 && s <= slices; s *= 2) {
-            const int64_t per = product_per((int)slices, s), parts = (slices + per - 1) / per, slots = (int64_t)IVFR_PRODUCT_CU * resident;
-            const double rounds = (double)((tiles * parts + slots - 1) / slots);
-            const double alone = resident > 1 && tiles * parts <= IVFR_PRODUCT_CU ? 0.75 : 1.0;   // a compute unit each
-            double cost = rounds * ((double)per * COSTS[k].slice[kind] * alone + COSTS[k].tile);
-            if (s > 1) cost += 6.0 + (double)parts * np * nq * 8.0 / 3.0e6;
-            if (cost < least) {
-                least = cost;
-                *tile = k;
-                *splits = (int)parts;
-            }
+    const int kind = planes == 1 ? 0 : planes == 3 ? 1 : 2, resident = COSTS[k].resident[kind];
+    if (!resident || (k == IVFR_TILE_128x16 && (q_outer || nq > 64))) return least;
+    const int64_t tiles = ((np + IVFR_TILE_P[k] - 1) / IVFR_TILE_P[k]) * ((nq + IVFR_TILE_Q[k] - 1) / IVFR_TILE_Q[k]);
+    for (int s = 1; s <= 128 && s <= slices; s *= 2) {
+        const int64_t per = product_per((int)slices, s), parts = (slices + per - 1) / per, slots = (int64_t)IVFR_PRODUCT_CU * resident;
+        const double rounds = (double)((tiles * parts + slots - 1) / slots);
+        const double alone = resident > 1 && tiles * parts <= IVFR_PRODUCT_CU ? 0.75 : 1.0;   // a compute unit each
+        double cost = rounds * ((double)per * COSTS[k].slice[kind] * alone + COSTS[k].tile);
+        if (s > 1) cost += 6.0 + (double)parts * np * nq * 8.0 / 3.0e6;
+        if (cost < least) {
+            least = cost;
+            *splits = (int)parts;
         }
+    }
+    return least;
+}
+
+// Each product by itself, or both with one tile, as one launch (see launch_both), which saves LAUNCH_US and fills the end of one with the start of the other.
+void product_cut(int64_t np, int64_t nq_x, int64_t slices_x, int64_t nq_w, int64_t slices_w, int planes, int* tile_x, int* splits_x, int* tile_w, int* splits_w) {
+    static const double LAUNCH_US = 8.0;
+    double x = 1e300, w = 1e300, both = 1e300;
+    int shared = 0, sx = 1, sw = 1;
+    for (int k = 0; k < IVFR_TILES; ++k) {
+        int px = 1, pw = 1;
+        const double cx = cut_with(k, np, nq_x, slices_x, planes, false, &px), cw = cut_with(k, np, nq_w, slices_w, planes, true, &pw);
+        if (cx < x) { x = cx; *tile_x = k; *splits_x = px; }
+        if (cw < w) { w = cw; *tile_w = k; *splits_w = pw; }
+        if ((k == IVFR_TILE_128x128 || k == IVFR_TILE_64x64) && cx + cw < both) { both = cx + cw; shared = k; sx = px; sw = pw; }
+    }
+    if (both - LAUNCH_US < x + w) {
+        *tile_x = *tile_w = shared;
+        *splits_x = sx;
+        *splits_w = sw;
     }
 }
 

@@ -472,8 +472,7 @@ static SoftmaxPlan softmax_plan(const ivfr_softmax_args& a, bool grad) {
         p.pieces = (int)((a.v + p.piece - 1) / p.piece);
         p.e_plane = (p.piece + 255) / 256 * p.n_pad * 256;
         p.at_e = take(p.e_planes * p.e_plane * 2);
-        product_cut(a.d, a.n, (p.piece + 31) / 32, p.planes_of_out, false, &p.dx_tile, &p.dx_splits);
-        product_cut(a.d, p.piece, p.n_pad / 32, p.planes_of_out, true, &p.dw_tile, &p.dw_splits);
+        product_cut(a.d, a.n, (p.piece + 31) / 32, p.piece, p.n_pad / 32, p.planes_of_out, &p.dx_tile, &p.dx_splits, &p.dw_tile, &p.dw_splits);
         if (p.pieces > 1 || p.dx_splits > 1) p.at_dx = take((int64_t)p.pieces * p.dx_splits * a.n * product_pad(a.d) * 4);
         if (p.dw_splits > 1) p.at_dw = take(p.dw_splits * p.piece * product_pad(a.d) * 4);
     }
