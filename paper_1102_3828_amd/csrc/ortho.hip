@@ -110,7 +110,7 @@ __device__ __forceinline__ void load_eight(const void* g, int64_t at, int align,
     }
 }
 
-// Sums of squares, in fp64 (squares of fp32 values need not fit fp32), in a fixed order.  Bound by reading g.
+// Sums of squares, in fp64 (squares of fp32 values need not fit fp32), in a fixed order.  Bound by reading g (4096 x 8192 in bf16: 42 us).
 template <bool F32>
 __global__ __launch_bounds__(256) void squares_kernel(MatrixArgs a) {
     __shared__ double red[4];
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(256) void squares_kernel(MatrixArgs a) {
     if (threadIdx.x == 0) a.sums[(int64_t)blockIdx.y * a.parts + blockIdx.x] = s;
 }
 
-// 64 x 64 values of X, through LDS where g is transposed
+// 64 x 64 values of X, through LDS where g is transposed.  Bound by the copy (4096 x 8192 in bf16: 42 us, 3.2 TB/s).
 __global__ __launch_bounds__(256) void fill_kernel(MatrixArgs a) {
     __shared__ float tile[64][65];
     __shared__ double red[4];
@@ -195,7 +195,8 @@ __device__ __forceinline__ void triangle(uint32_t t, int& p, int& q) {
     q = __builtin_amdgcn_readfirstlane((int)(t - (uint32_t)i * (i + 1) / 2));
 }
 
-// A = X X^T / scale, or B = first A + second A A^T
+// A = X X^T / scale, or B = first A + second A A^T: the lower triangle of tiles, stored twice.  Bound by the compute units that the triangle gives work: of
+// 4096 x 8192 in bf16 136 tiles for 256 compute units, 209 us (0.70 PFLOP/s of what is formed), B of it 116.
 template <class C, bool SQUARE>
 __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void gram_kernel(StepArgs a) {
     __shared__ __align__(1024) char smem[C::LDS];
@@ -213,46 +214,47 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void gram_kernel(StepArg
         w.p_at = w.q_at = (int64_t)w.split * a.planes * size;
         return true;
     }, [&](const ProductWork& tile, floatx4 (&acc)[C::TM][C::TN]) {
-    const int tid = C::thread(), tp = tile.p, tq = tile.q, p0 = tp * C::BM, q0 = tq * C::BN;
-    const uint16_t* const src = src0 + tile.p_at;
-    uint16_t* const y = a.y + (int64_t)tile.split * a.planes * a.asize;
+        const int tid = C::thread(), tp = tile.p, tq = tile.q, p0 = tp * C::BM, q0 = tq * C::BN;
+        const uint16_t* const src = src0 + tile.p_at;
+        uint16_t* const y = a.y + (int64_t)tile.split * a.planes * a.asize;
 #pragma unroll
-    for (int u = 0; u < C::TN; ++u) {
-        const int q = q0 + C::q_of(tid, u);
-        if (q >= a.rp) continue;
+        for (int u = 0; u < C::TN; ++u) {
+            const int q = q0 + C::q_of(tid, u);
+            if (q >= a.rp) continue;
 #pragma unroll
-        for (int t = 0; t < C::TM; t += 2) {
-            const int p = p0 + C::p_of(tid, t);
-            if (p >= a.rp) continue;   // (a multiple of 8, as p)
-            float v[8];
+            for (int t = 0; t < C::TM; t += 2) {
+                const int p = p0 + C::p_of(tid, t);
+                if (p >= a.rp) continue;   // (a multiple of 8, as p)
+                float v[8];
 #pragma unroll
-            for (int r = 0; r < 8; ++r) v[r] = a.second * acc[t + (r >> 2)][u][r & 3];
-            const int64_t at = (int64_t)q * a.ald + p;
-            if constexpr (SQUARE) {
-                const half8v h = *reinterpret_cast<const half8v*>(src + at);
-                half8v l = {0, 0, 0, 0, 0, 0, 0, 0};
-                if (a.planes > 1) l = *reinterpret_cast<const half8v*>(src + a.asize + at);
+                for (int r = 0; r < 8; ++r) v[r] = a.second * acc[t + (r >> 2)][u][r & 3];
+                const int64_t at = (int64_t)q * a.ald + p;
+                if constexpr (SQUARE) {
+                    const half8v h = *reinterpret_cast<const half8v*>(src + at);
+                    half8v l = {0, 0, 0, 0, 0, 0, 0, 0};
+                    if (a.planes > 1) l = *reinterpret_cast<const half8v*>(src + a.asize + at);
 #pragma unroll
-                for (int r = 0; r < 8; ++r) v[r] += a.first * ((float)h[r] + (float)l[r]);
-            }
-#pragma unroll
-            for (int n = 0; n < C::PLANES; ++n) {
-                uint16_t* const o = y + n * a.asize;
-                short8v h;
-#pragma unroll
-                for (int r = 0; r < 8; ++r) {
-                    const uint16_t b = to_half(v[r]);
-                    h[r] = (short)b;
-                    v[r] -= from_half(b);
-                    if (tp != tq) o[(int64_t)(p + r) * a.ald + q] = b;
+                    for (int r = 0; r < 8; ++r) v[r] += a.first * ((float)h[r] + (float)l[r]);
                 }
-                *reinterpret_cast<short8v*>(o + at) = h;
+#pragma unroll
+                for (int n = 0; n < C::PLANES; ++n) {
+                    uint16_t* const o = y + n * a.asize;
+                    short8v h;
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        const uint16_t b = to_half(v[r]);
+                        h[r] = (short)b;
+                        v[r] -= from_half(b);
+                        if (tp != tq) o[(int64_t)(p + r) * a.ald + q] = b;
+                    }
+                    *reinterpret_cast<short8v*>(o + at) = h;
+                }
             }
         }
-    }    });
+    });
 }
 
-// X <- first X + second B X
+// X <- first X + second B X, X's planes read again where the products end.  Bound by the matrix cores and their power: 4096 x 8192 in bf16 273 us, 1.01 PFLOP/s.
 template <class C>
 __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void update_kernel(StepArgs a) {
     __shared__ __align__(1024) char smem[C::LDS];
@@ -265,50 +267,52 @@ __global__ __launch_bounds__(C::THREADS, C::WAVES_SIMD) void update_kernel(StepA
         w.q_at = (int64_t)w.split * a.planes * a.asize;
         return true;
     }, [&](const ProductWork& tile, floatx4 (&acc)[C::TM][C::TN]) {
-    const int tid = C::thread(), p0 = tile.p * C::BM, q0 = tile.q * C::BN;
-    const uint16_t* const x = a.x + tile.p_at;
-    uint16_t* const y = a.y + tile.p_at;
+        const int tid = C::thread(), p0 = tile.p * C::BM, q0 = tile.q * C::BN;
+        const uint16_t* const x = a.x + tile.p_at;
+        uint16_t* const y = a.y + tile.p_at;
 #pragma unroll
-    for (int u = 0; u < C::TN; ++u) {
-        const int q = q0 + C::q_of(tid, u);
-        if (q >= a.rp) continue;
+        for (int u = 0; u < C::TN; ++u) {
+            const int q = q0 + C::q_of(tid, u);
+            if (q >= a.rp) continue;
 #pragma unroll
-        for (int t = 0; t < C::TM; ++t) {
-            const int p = p0 + C::p_of(tid, t);
-            if (p >= a.cp) continue;   // (a multiple of 4, as p)
-            const int64_t at = (int64_t)q * a.xld + p;
-            const half4v h = *reinterpret_cast<const half4v*>(x + at);
-            half4v l = {0, 0, 0, 0};
-            if (a.planes > 1) l = *reinterpret_cast<const half4v*>(x + a.xsize + at);
-            float v[4];
+            for (int t = 0; t < C::TM; ++t) {
+                const int p = p0 + C::p_of(tid, t);
+                if (p >= a.cp) continue;   // (a multiple of 4, as p)
+                const int64_t at = (int64_t)q * a.xld + p;
+                const half4v h = *reinterpret_cast<const half4v*>(x + at);
+                half4v l = {0, 0, 0, 0};
+                if (a.planes > 1) l = *reinterpret_cast<const half4v*>(x + a.xsize + at);
+                float v[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = fmaf(a.first, (float)h[r] + (float)l[r], a.second * acc[t][u][r]);
-            if (a.out) {
-                if (q >= a.rows) continue;
-                const int64_t o = ((int64_t)tile.split * a.rows + q) * a.cols + p;
+                for (int r = 0; r < 4; ++r) v[r] = fmaf(a.first, (float)h[r] + (float)l[r], a.second * acc[t][u][r]);
+                if (a.out) {
+                    if (q >= a.rows) continue;
+                    const int64_t o = ((int64_t)tile.split * a.rows + q) * a.cols + p;
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (p + r < a.cols) store_value(a.out, o + r, a.type, v[r] * a.out_scale);
-            } else {
-                half4v n;
+                    for (int r = 0; r < 4; ++r)
+                        if (p + r < a.cols) store_value(a.out, o + r, a.type, v[r] * a.out_scale);
+                } else {
+                    half4v n;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) n[r] = (_Float16)v[r];
-                *reinterpret_cast<half4v*>(y + at) = n;
-                if (a.planes > 1) {
+                    for (int r = 0; r < 4; ++r) n[r] = (_Float16)v[r];
+                    *reinterpret_cast<half4v*>(y + at) = n;
+                    if (a.planes > 1) {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) n[r] = (_Float16)(v[r] - (float)n[r]);
-                    *reinterpret_cast<half4v*>(y + a.xsize + at) = n;
+                        for (int r = 0; r < 4; ++r) n[r] = (_Float16)(v[r] - (float)n[r]);
+                        *reinterpret_cast<half4v*>(y + a.xsize + at) = n;
+                    }
                 }
             }
         }
-    }    });
+    });
 }
 
 // ---------------------------------------------------------------- small matrices
 
 // All steps of a matrix in one workgroup, X and A (then B, in its place) in LDS: no launch and no memory in between.  A wavefront has
 // sixteen rows of the outputs and blocks of 32 of their columns (with fewer than 128 rows several wavefronts share the columns of the same rows), so
-// that it reads a fragment of its rows once for all blocks; results stay in registers until all have read what they replace.
+// that it reads a fragment of its rows once for all blocks; results stay in registers until all have read what they replace.  Bound by LDS reads and the barriers
+// between the products, on one compute unit a matrix: 128 x 128 44 us, sixteen of 64 x 500 45 us (a launch for every product: 90 and 101).
 // A matrix lies in LDS as slices of 32 columns, rows of 64 bytes, the four 16-byte chunks of a row permuted by its number: the lanes that are served together,
 // of eight rows (0-3 and 8-11: a wavefront's sixteen rows are every other four of 32) or, transposed, of four and four rows, meet different banks.
 #define SMALL_BLOCKS 8         // that a wavefront holds at most

@@ -5,7 +5,8 @@
 // Several 16-bit planes carry one fp32 operand (its leading part, what that leaves, what that leaves again); the product is then the sum
 // over pairs of planes, on the same accumulators.
 //
-// A workgroup owns BM x BN outputs.  Stages of KSUB x 32 k go straight from memory to LDS, STAGES buffers, all of them in flight but
+// A workgroup owns BM x BN outputs of one tile after another.  Stages of KSUB x 32 k (64: whole lines of 128 bytes of an inner operand; with half lines the
+// larger tiles took twice the traffic from L2) go straight from memory to LDS, STAGES buffers, all of them in flight but
 // the one in use; one barrier a stage.  The fragments of a slice of 32 are read from LDS into registers while the products of the slice before
 // are formed.  16-byte chunks of a row lie permuted in LDS (by the row, as the source addresses choose), so that the lanes that LDS serves
 // together read different banks; outer operands are transposed by the LDS read itself (ds_read_b64_tr_b16).
@@ -37,8 +38,8 @@ struct ProductOperand {
     // rows of a hundred KB would spread a tile over as many pages as it has rows.
     int64_t panel = 256;
 };
-// Elements between the rows of an operand that is laid out here: whole lines of 128 bytes (with rows that begin inside a line every stage reads lines by halves: 8 % more time)
 #define IVFR_PRODUCT_WHOLE (1 << 30)   // rows, of an operand that is padded with zeros to whole slices
+// Elements between the rows of an operand that is laid out here: whole lines of 128 bytes (with rows that begin inside a line every stage reads lines by halves: 8 % more time)
 inline int64_t product_ld(int64_t k) { return (k + 63) / 64 * 64; }
 
 // What a workgroup computes of a launch's tiles: the i-th tile of workgroup `block` of `blocks`.  XCDs take contiguous runs of tiles (blocks go round the
