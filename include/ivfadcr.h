@@ -261,7 +261,8 @@ int ivfr_stage_times(const ivfr_index* index, double* ms, int32_t* scan_launches
  * must not overlap.  Calls are enqueued on `stream` and return without waiting; nothing is allocated or read back, so they can
  * be captured in a graph, and calls with different workspaces may overlap.  *_workspace is host arithmetic: the bytes that
  * the call with these arguments needs (aligned to 256).  Matrices are row-major with a leading dimension in elements; inputs
- * may start anywhere that their type allows (rows of 16-byte alignment are read in place, others copied).
+ * may start anywhere that their type allows (rows of 16-byte alignment are read in place, others copied;
+ * gradients copy x).
  * Sums and statistics are fp32.  Products of bf16 and fp16 inputs are exact; fp32 inputs are split into three bf16 parts, whose
  * six leading products neglect 2^-24 of a product.  Errors: IVFR_ERR_INVALID_ARG, IVFR_ERR_HIP. */
 #define IVFR_TYPE_F32  0
@@ -279,7 +280,8 @@ int ivfr_stage_times(const ivfr_index* index, double* ms, int32_t* scan_launches
  * ivfr_softmax_loss: loss, lse fp32 [n].
  * ivfr_softmax_loss_grad: weight fp32 [n], the gradient of each row's loss; lse fp32 [n] of ivfr_softmax_loss for these arguments (or of a larger
  * set), or NULL: it is then formed here, as in fp32 calls always (a number of 24 bits says too little of a target with nearly all of the probability).
- * e is rounded to the inputs' type where it enters the products of bf16 and fp16 calls with more than 512 rows, to twice its bits with fewer; loss fp32 [n], or NULL; dx [n, d] and dw [v, d] dense, of the inputs' type, aligned to 16 bytes.
+ * e is rounded to the inputs' type where it enters the products of bf16 and fp16 calls with more than 512 rows, to twice its bits with fewer;
+ * loss fp32 [n], or NULL; dx [n, d] and dw [v, d] dense, of the inputs' type, aligned to 16 bytes.
  * fp16 gradients below 2^-24 are zero in that type: scale the weights as for any training in fp16.  The order of every sum is fixed:
  * the same call gives the same bits. */
 typedef struct {
